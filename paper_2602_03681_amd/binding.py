@@ -77,7 +77,9 @@ EXPORTS = ("nats_hybrid_attn_fwd_workspace_bytes", "nats_hybrid_attn_fwd", "nats
            "nats_hybrid_attn_decode_chunk", "nats_hybrid_attn_decode_commit", "nats_merge_weights", "nats_route_chunks",
            "nats_hybrid_attn_bwd_workspace_bytes", "nats_hybrid_attn_bwd", "nats_hybrid_attn_bwd_bf16",
            "nats_hybrid_attn_fwd_noalloc",
-           "nats_hybrid_attn_decode_workspace_bytes", "nats_merge_weights_from_x")
+           "nats_hybrid_attn_decode_workspace_bytes", "nats_merge_weights_from_x",
+           "nats_hybrid_attn_decode_tree_workspace_bytes", "nats_hybrid_attn_decode_tree", "nats_hybrid_attn_tree_commit",
+           "nats_cache_weights_workspace_bytes", "nats_cache_weights", "nats_cache_evict")
 
 
 def library_path() -> str:
@@ -141,6 +143,8 @@ def load_library():
     lib.nats_profile_end.restype = ctypes.c_int
     lib.nats_profile_end.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_float),
                                      ctypes.POINTER(ctypes.c_int32), ctypes.c_int]
+    from . import serve   # the entry points of nats_serve.h
+    serve.declare(lib)
     _lib = lib
     return lib
 

@@ -1,0 +1,66 @@
+// Resolved calls of the operators of nats_serve.h, handed to the kernels (internal header).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "nats_serve.h"
+
+namespace nats {
+
+struct TreeCall {
+    int B, H, G, T, d, cap, dtype;
+    float scale, la_scale, eps;
+    int combine_mode, linear_op, freeze;
+    const float* state;
+    const void *k_cache, *v_cache;
+    const int32_t* cache_len;
+    const void *q, *k, *v, *q_nla, *k_nla;
+    const float *alpha, *beta;
+    const uint8_t* mask;
+    const int32_t *parent, *n_nodes;
+    const float *w_nla, *w_la;
+    void* o;
+    float* lse;
+    float* ws;
+    int n_split;                       // parts of a cache
+    size_t off_ola, off_u, off_part;   // floats
+};
+size_t tree_workspace(TreeCall& c);    // floats; fills n_split and the offsets
+nats_status launch_tree(const TreeCall& c, hipStream_t st);
+
+struct TreeCommitCall {
+    int B, H, G, T, d, cap, dtype;
+    int linear_op, freeze;
+    float* state;
+    void *k_cache, *v_cache;
+    int32_t* cache_len;
+    const void *k, *v, *k_nla;
+    const float *alpha, *beta;
+    const uint8_t* mask;
+    const int32_t *parent, *node;
+    int32_t *vis, *err_flags;
+};
+nats_status launch_tree_commit(const TreeCommitCall& c, hipStream_t st);
+
+struct WeightsCall {
+    int B, H, T, d, cap, dtype, q_group, vis_group;
+    float scale, decay;
+    float* weights;
+    const void *q, *k_cache;
+    const int32_t *cache_len, *vis;
+    const float* lse;
+    float* ws;
+};
+size_t weights_workspace(const WeightsCall& c, bool lse_given);   // floats
+nats_status launch_cache_weights(const WeightsCall& c, hipStream_t st);
+
+struct EvictCall {
+    int B, H, d, cap, dtype, keep, recent;
+    void *k_cache, *v_cache;
+    int32_t* cache_len;
+    float* weights;
+    int32_t* kept;
+};
+nats_status launch_cache_evict(const EvictCall& c, hipStream_t st);
+
+}  // namespace nats
