@@ -22,11 +22,13 @@ struct TreeCall {
     void* o;
     float* lse;
     float* ws;
-    int n_split;                       // parts of a cache
-    size_t off_ola, off_u, off_part;   // floats
+    int rows, n_split;                         // rows of a part, parts of a cache
+    size_t off_ola, off_u, off_part, off_ml;   // floats
 };
-size_t tree_workspace(TreeCall& c);    // floats; fills n_split and the offsets
+size_t tree_workspace(TreeCall& c);    // floats; fills rows, n_split and the offsets
 nats_status launch_tree(const TreeCall& c, hipStream_t st);
+int tree_cache_rows(const TreeCall& c);
+nats_status launch_tree_cache(const TreeCall& c, hipStream_t st);
 
 struct TreeCommitCall {
     int B, H, G, T, d, cap, dtype;

@@ -98,117 +98,110 @@ __global__ __launch_bounds__(D) void tree_linear_kernel(TreeCall c) {
     }
 }
 
-// ---- softmax branch: partial results (m, l, sum of weighted rows) of TREE_ROWS cache rows for one node ----
-constexpr int TREE_ROWS = 256;
+// ---- the parts, the node's softmax ancestors and the linear branch's row into the output: a wavefront per node and head ----
+constexpr int MERGE_THREADS = 256;
 
 template <typename T, int D>
-__global__ __launch_bounds__(TREE_ROWS) void tree_cache_kernel(TreeCall c) {
-    __shared__ float s_p[TREE_ROWS], s_q[D], s_red[8], s_acc[TREE_ROWS / D][D];
-    const int t = blockIdx.x, split = blockIdx.y, bhg = blockIdx.z, tid = threadIdx.x, N = c.T;
-    const int n = min(max(c.cache_len[bhg], 0), c.cap), lo = split * TREE_ROWS, here = min(n - lo, TREE_ROWS);
-    if (here <= 0) return;
-    const T* q = c.q_nla != nullptr ? (const T*)c.q_nla + ((size_t)bhg * N + t) * D : (const T*)c.q + ((size_t)(bhg / c.G) * N + t) * D;
-    if (tid < D) s_q[tid] = to_float(q[tid]) * c.scale;
-    __syncthreads();
-    const T* K = (const T*)c.k_cache + ((size_t)bhg * c.cap + lo) * D;
-    const T* V = (const T*)c.v_cache + ((size_t)bhg * c.cap + lo) * D;
-    float x = -INFINITY;
-    if (tid < here) {
-        x = 0.f;
-        for (int e = 0; e < D; ++e) x += s_q[e] * to_float(K[(size_t)tid * D + e]);
-    }
-    float m = x;
-    for (int w = 1; w < 64; w *= 2) m = fmaxf(m, __shfl_xor(m, w));
-    if ((tid & 63) == 0) s_red[tid >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    const float ref = m == -INFINITY ? 0.f : m;
-    const float p = tid < here ? expf(x - ref) : 0.f;
-    s_p[tid] = p;
-    const float l = lane_group_sum<64>(p);
-    if ((tid & 63) == 0) s_red[4 + (tid >> 6)] = l;
-    __syncthreads();
-    const int col = tid % D, part = tid / D;
-    float acc = 0.f;
-    for (int r = part; r < here; r += TREE_ROWS / D) acc += s_p[r] * to_float(V[(size_t)r * D + col]);
-    s_acc[part][col] = acc;
-    __syncthreads();
-    float* out = c.ws + c.off_part + (((size_t)bhg * c.n_split + split) * N + t) * (D + 2);
-    if (tid < D) {
-        acc = 0.f;
-        for (int i = 0; i < TREE_ROWS / D; ++i) acc += s_acc[i][tid];
-        out[2 + tid] = acc;
-        if (tid == 0) {
-            out[0] = m;
-            out[1] = s_red[4] + s_red[5] + s_red[6] + s_red[7];
-        }
-    }
-}
-
-// ---- the parts, the node's softmax ancestors and the linear branch's row into the output: a block per node and head ----
-template <typename T, int D>
-__global__ __launch_bounds__(D) void tree_merge_kernel(TreeCall c) {
-    __shared__ float s_red[4];
-    __shared__ uint64_t s_sees;
-    const int t = blockIdx.x, bhg = blockIdx.y, bh = bhg / c.G, b = bh / c.H, tid = threadIdx.x, N = c.T;
-    auto block_sum = [&](float x) {
-        x = lane_group_sum<64>(x);
-        __syncthreads();
-        if ((tid & 63) == 0) s_red[tid >> 6] = x;
-        __syncthreads();
-        return D > 64 ? s_red[0] + s_red[1] : s_red[0];
+__global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
+    constexpr int CPL = D / 64;   // columns per lane, side by side
+    const int lane = threadIdx.x & 63, bhg = blockIdx.y, bh = bhg / c.G, b = bh / c.H, N = c.T;
+    const int t = blockIdx.x * (MERGE_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (t >= N) return;
+    const size_t at = (size_t)bhg * N + t;
+    auto columns = [&](const T* row, float (&x)[CPL]) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) x[i] = to_float(row[lane * CPL + i]);
     };
-    T* o = (T*)c.o + ((size_t)bhg * N + t) * D;
+    auto store = [&](const float (&x)[CPL]) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) ((T*)c.o)[at * D + lane * CPL + i] = from_float<T>(x[i]);
+    };
+    float res[CPL] = {};
     if (c.n_nodes != nullptr && t >= c.n_nodes[b]) {
-        o[tid] = from_float<T>(0.f);
-        if (tid == 0 && c.lse != nullptr) c.lse[(size_t)bhg * N + t] = -INFINITY;
+        store(res);
+        if (lane == 0 && c.lse != nullptr) c.lse[at] = -INFINITY;
         return;
     }
-    if (tid < 64) {
-        uint64_t anc = ancestors(parent_of(c.parent, b, N, tid), tid);
-        const uint64_t soft = __ballot(tid < N && c.mask[(size_t)bh * N + min(tid, N - 1)] != 0);
-        if (tid == t) s_sees = anc & soft;
-    }
-    __syncthreads();
-    const T* qs = c.q_nla != nullptr ? (const T*)c.q_nla + (size_t)bhg * N * D : (const T*)c.q + (size_t)bh * N * D;
+    const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
+    const uint64_t soft = __ballot(lane < N && c.mask[(size_t)bh * N + min(lane, N - 1)] != 0);
+    const uint64_t anc = ancestors(parent_of(c.parent, b, N, lane), lane);
+    const uint64_t sees = soft & (((uint64_t)(uint32_t)__shfl((int)(uint32_t)(anc >> 32), t) << 32) | (uint32_t)__shfl((int)(uint32_t)anc, t));
+    // the nodes' logits, lane j for node j, in the parts' units (powers of 2)
+    constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : (const T*)c.k + (size_t)bh * N * D;
     const T* v = (const T*)c.v + (size_t)bhg * N * D;
-    const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + TREE_ROWS - 1) / TREE_ROWS;
-    float m = -INFINITY, l = 0.f, acc = 0.f;
-    auto fold = [&](float m2, float l2, float acc2) {
-        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-        const float w1 = expf(m - ref), w2 = expf(m2 - ref);
-        l = w1 * l + w2 * l2;
-        acc = w1 * acc + w2 * acc2;
-        m = top;
+    float q[CPL], x = -INFINITY;
+    columns(c.q_nla != nullptr ? (const T*)c.q_nla + at * D : (const T*)c.q + ((size_t)bh * N + t) * D, q);
+    for (uint64_t left = sees; left; left &= left - 1) {
+        const int j = __builtin_ctzll(left);
+        float k[CPL], dot = 0.f;
+        columns(ks + (size_t)j * D, k);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) dot += q[i] * k[i];
+        dot = lane_group_sum<64>(dot);
+        if (lane == j) x = dot * (c.scale * LOG2E);
+    }
+    auto top_of = [](float y) {
+#pragma unroll
+        for (int w = 1; w < 64; w *= 2) y = fmaxf(y, __shfl_xor(y, w));
+        return y;
     };
-    for (int s = 0; s < parts; ++s) {
-        const float* part = c.ws + c.off_part + (((size_t)bhg * c.n_split + s) * N + t) * (D + 2);
-        fold(part[0], part[1], part[2 + tid]);
+    const bool mine = (sees >> lane) & 1;
+    float m = top_of(x), ref = m == -INFINITY ? 0.f : m;
+    float p = mine ? __builtin_amdgcn_exp2f(x - ref) : 0.f, l = lane_group_sum<64>(p), acc[CPL] = {};
+    for (uint64_t left = sees; left; left &= left - 1) {
+        const int j = __builtin_ctzll(left);
+        float vj[CPL];
+        columns(v + (size_t)j * D, vj);
+        const float pj = __shfl(p, j);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) acc[i] += pj * vj[i];
     }
-    for (uint64_t x = s_sees; x; x &= x - 1) {
-        const int j = __builtin_ctzll(x);
-        const float dot = block_sum(to_float(qs[t * D + tid]) * c.scale * to_float(ks[j * D + tid]));
-        fold(dot, 1.f, to_float(v[j * D + tid]));
-    }
-    const bool none = n == 0 && s_sees == 0;
-    const float o_nla = none ? 0.f : acc / l;
-    const float o_la = c.ws[c.off_ola + ((size_t)bhg * N + t) * D + tid];
-    if (tid == 0 && c.lse != nullptr) c.lse[(size_t)bhg * N + t] = none ? -INFINITY : m + logf(l);
-    float res = o_la + o_nla;
-    if (c.combine_mode != 0) {
-        const float def = c.combine_mode == 1 ? 0.5f : 1.f;
-        const float wn = c.w_nla != nullptr ? c.w_nla[(size_t)bhg * N + t] : def;
-        const float wl = c.w_la != nullptr ? c.w_la[(size_t)bhg * N + t] : def;
-        if (c.combine_mode == 1) {
-            const float sn = block_sum(o_nla * o_nla), sl = block_sum(o_la * o_la);
-            res = wn * o_nla / sqrtf(sn / D + c.eps) + wl * o_la / sqrtf(sl / D + c.eps);
-        } else {
-            res = wn * o_nla + wl * o_la;
-            res = res / sqrtf(block_sum(res * res) / D + c.eps);
+    for (int first = 0; first < parts; first += 64) {
+        const size_t part = ((size_t)bhg * c.n_split + first) * N + t;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (first + lane < parts) ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part + (size_t)lane * N) * 2);
+        const float top = fmaxf(m, top_of(ml.x));
+        ref = top == -INFINITY ? 0.f : top;
+        const float was = __builtin_amdgcn_exp2f(m - ref), w = __builtin_amdgcn_exp2f(ml.x - ref);
+        m = top;
+        l = l * was + lane_group_sum<64>(first + lane < parts ? w * ml.y : 0.f);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) acc[i] *= was;
+        const float* rows = c.ws + c.off_part + part * D + lane * CPL;
+        const int here = min(parts - first, 64);
+#pragma unroll 8
+        for (int s = 0; s < here; ++s) {
+            const float ws = __shfl(w, s);
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) acc[i] += ws * rows[(size_t)s * N * D + i];
         }
     }
-    o[tid] = from_float<T>(res);
+    const bool none = n == 0 && sees == 0;
+    if (lane == 0 && c.lse != nullptr) c.lse[at] = none ? -INFINITY : (m + log2f(l)) * LN2;
+    float o_nla[CPL], o_la[CPL];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) {
+        o_nla[i] = none ? 0.f : acc[i] / l;
+        o_la[i] = c.ws[c.off_ola + at * D + lane * CPL + i];
+        res[i] = o_la[i] + o_nla[i];
+    }
+    if (c.combine_mode != 0) {
+        const float def = c.combine_mode == 1 ? 0.5f : 1.f;
+        const float wn = c.w_nla != nullptr ? c.w_nla[at] : def, wl = c.w_la != nullptr ? c.w_la[at] : def;
+        float sn = 0.f, sl = 0.f;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            res[i] = wn * o_nla[i] + wl * o_la[i];
+            sn += c.combine_mode == 1 ? o_nla[i] * o_nla[i] : res[i] * res[i];
+            sl += o_la[i] * o_la[i];
+        }
+        sn = sqrtf(lane_group_sum<64>(sn) / D + c.eps);
+        sl = sqrtf(lane_group_sum<64>(sl) / D + c.eps);
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) res[i] = c.combine_mode == 1 ? wn * o_nla[i] / sn + wl * o_la[i] / sl : res[i] / sn;
+    }
+    store(res);
 }
 
 // ---- commit: a block per output head; LPR = D / 4 lanes hold a row of S as a float4 each, the rows of S are independent of one
@@ -287,13 +280,15 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
 }
 
 // ---- host side ----
-size_t tree_workspace(TreeCall& c) {   // floats; fills the offsets
+size_t tree_workspace(TreeCall& c) {
     const size_t heads = (size_t)c.B * c.H * c.G;
-    c.n_split = (c.cap + TREE_ROWS - 1) / TREE_ROWS;
+    c.rows = tree_cache_rows(c);
+    c.n_split = (c.cap + c.rows - 1) / c.rows;
     c.off_ola = 0;
     c.off_u = heads * c.T * c.d;
     c.off_part = 2 * heads * c.T * c.d;
-    return c.off_part + heads * c.n_split * c.T * (c.d + 2);
+    c.off_ml = c.off_part + heads * c.n_split * c.T * c.d;
+    return c.off_ml + heads * c.n_split * c.T * 2;
 }
 
 template <typename T, int D>
@@ -303,12 +298,11 @@ static nats_status run_tree(const TreeCall& c, hipStream_t st) {
         ProfScope ps("tree_linear", st);
         hipLaunchKernelGGL((tree_linear_kernel<T, D>), dim3(heads), dim3(D), 0, st, c);
     }
-    {
-        ProfScope ps("tree_cache", st);
-        hipLaunchKernelGGL((tree_cache_kernel<T, D>), dim3(c.T, c.n_split, heads), dim3(TREE_ROWS), 0, st, c);
-    }
+    const nats_status r = launch_tree_cache(c, st);
+    if (r != NATS_OK) return r;
+    constexpr int NODES = MERGE_THREADS / 64;
     ProfScope ps("tree_merge", st);
-    hipLaunchKernelGGL((tree_merge_kernel<T, D>), dim3(c.T, heads), dim3(D), 0, st, c);
+    hipLaunchKernelGGL((tree_merge_kernel<T, D>), dim3((c.T + NODES - 1) / NODES, heads), dim3(MERGE_THREADS), 0, st, c);
     return check_launch("tree");
 }
 

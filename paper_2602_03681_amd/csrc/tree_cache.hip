@@ -1,0 +1,334 @@
+// Softmax branch of a tree of drafted tokens over the cache: partial results (running maximum m, sum l, weighted sum of V rows) of up to
+// 64 queries over a part of a cache's rows.
+//
+// Memory-bound: a cache row of 4 d (bf16) or 8 d bytes (fp32) feeds 4 d T operations, at most T = 64 per byte, against the 240 (bf16)
+// that a large product has per byte of a large copy on this card.  So all that matters is that every row is read once and that enough
+// loads are in flight: a wavefront takes tiles of 32 rows (fp32: 16) by itself, holds a tile of K and one of V in registers, and asks
+// for the next K as soon as the logits are there, for the next V as soon as it has been put in order, so that the softmax and
+// the second product run while 16 KB per wavefront are on their way.  No LDS in the loop, no barrier.
+//
+//   S^T [key x query] = K Q^T      A = K rows as they lie in memory (16 bytes per lane), B = Q, in registers throughout
+//   O^T [d_v x query] += V^T P^T   B = P^T as the first product's result tiles hold it (a lane has 4 consecutive keys of one query, two
+//                                  tiles fill the 8 slots of a bf16 operand); A = V^T: a lane reads 8 (4) columns of the keys of
+//                                  its slots, and column 8 l + e of all lanes l is row l of tile e: the keys' halves of a column are
+//                                  joined by byte permutes (bf16) or stand as they came (fp32)
+// bf16 tensors: logits are exact products summed in fp32; P enters as the sum of two bf16 terms (17 bits), for one term (8 bits) would
+// show in fp32 outputs' accuracy and this kernel has matrix cycles to spare.  The upper term is cut off and the lower one kept above 0, so that
+// an infinity in V stays one.
+#include <math.h>
+
+#include "mfma_util.h"
+#include "nats_common.h"
+#include "serve.h"
+
+namespace nats {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+// over the lanes l, l ^ 16, l ^ 32, l ^ 48, which share a query
+__device__ __forceinline__ float over_quads_max(float x) {
+    const int lane = threadIdx.x & 63;
+    x = fmaxf(x, lane_xor32(x, lane));
+    return fmaxf(x, lane_xor16(x, lane));
+}
+__device__ __forceinline__ float over_quads_sum(float x) {
+    const int lane = threadIdx.x & 63;
+    x += lane_xor32(x, lane);
+    return x + lane_xor16(x, lane);
+}
+
+// A tile of 16 KT rows in a wavefront's registers, and the two products with it.
+template <typename T, int D>
+struct CacheTile;
+
+template <int D>
+struct CacheTile<bf16_t, D> {
+    static constexpr int KT = 2, W = D / 32;   // W: 32-bit words of a V row per lane (D / 16 columns)
+    using Query = u32x4[D / 32];               // column l16 of Q^T, elements 32 ks + 8 lq ..
+    using Weights = u32x4[2];                  // upper and lower terms
+    u32x4 k[KT][D / 32];
+    uint32_t v[8][W];                          // slot s: key 16 (s / 4) + 4 lq + s % 4
+    __device__ __forceinline__ static void load_query(const bf16_t* row, int lq, bool live, Query& q) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+            q[i] = live ? *reinterpret_cast<const u32x4*>(row + 32 * i + 8 * lq) : u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void load_k(const bf16_t* K, int row, int last, int l16, int lq) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            const bf16_t* p = K + (size_t)min(row + 16 * t + l16, last) * D + 8 * lq;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) k[t][i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
+        }
+    }
+    __device__ __forceinline__ void load_v(const bf16_t* V, int row, int last, int l16, int lq) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const bf16_t* p = V + (size_t)min(row + 16 * (s / 4) + 4 * lq + s % 4, last) * D + 2 * W * l16;
+            if constexpr (W == 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[s][i] = x[i];
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(p);
+                v[s][0] = x.x;
+                v[s][1] = x.y;
+            }
+        }
+    }
+    __device__ __forceinline__ void clear_v(int row, int last, int lq) {   // rows past the last one may hold anything
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[s][i] = row + 16 * (s / 4) + 4 * lq + s % 4 > last ? 0u : v[s][i];
+    }
+    __device__ __forceinline__ void logits(const Query& q, f32x4 (&s)[KT]) const {
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) s[t] = mfma_bf16(k[t][i], q[i], s[t]);
+        }
+    }
+    __device__ __forceinline__ static void weights(const f32x4 (&p)[KT], Weights& w) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
+            const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
+            w[0][i] = (hx >> 16) | hy;
+            w[1][i] = pack_bf16x2(fmaxf(x - __uint_as_float(hx), 0x1p-120f), fmaxf(y - __uint_as_float(hy), 0x1p-120f));
+        }
+    }
+    // column `column(lq, j, e)` of the result is what element j of tile e holds
+    __device__ __forceinline__ static int column(int lq, int j, int e) { return 2 * W * (4 * lq + j) + e; }
+    template <int NQ>
+    __device__ __forceinline__ void products(const Weights (&w)[NQ], f32x4 (&o)[NQ][D / 16]) const {
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {
+            u32x4 a;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                o[n][e] = mfma_bf16(a, w[n][0], o[n][e]);
+                o[n][e] = mfma_bf16(a, w[n][1], o[n][e]);
+            }
+        }
+    }
+};
+
+template <int D>
+struct CacheTile<float, D> {
+    static constexpr int KT = 1;
+    using Query = float4[D / 16];
+    using Weights = f32x4[1];
+    float4 k[D / 16];
+    float4 v[4][D / 64];   // key 4 lq + j, columns 64 g + 4 l16 ..
+    __device__ __forceinline__ static void load_query(const float* row, int lq, bool live, Query& q) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i] = live ? ld4(row + 16 * i + 4 * lq) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ __forceinline__ void load_k(const float* K, int row, int last, int l16, int lq) {
+        const float* p = K + (size_t)min(row + l16, last) * D + 4 * lq;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) k[i] = ld4(p + 16 * i);
+    }
+    __device__ __forceinline__ void load_v(const float* V, int row, int last, int l16, int lq) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int g = 0; g < D / 64; ++g) v[j][g] = ld4(V + (size_t)min(row + 4 * lq + j, last) * D + 64 * g + 4 * l16);
+    }
+    __device__ __forceinline__ void clear_v(int row, int last, int lq) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int g = 0; g < D / 64; ++g) {
+                const bool out = row + 4 * lq + j > last;
+                v[j][g].x = out ? 0.f : v[j][g].x;
+                v[j][g].y = out ? 0.f : v[j][g].y;
+                v[j][g].z = out ? 0.f : v[j][g].z;
+                v[j][g].w = out ? 0.f : v[j][g].w;
+            }
+    }
+    __device__ __forceinline__ void logits(const Query& q, f32x4 (&s)[KT]) const {
+        s[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) s[0] = mac16(k[i], q[i], s[0]);
+    }
+    __device__ __forceinline__ static void weights(const f32x4 (&p)[KT], Weights& w) { w[0] = p[0]; }
+    __device__ __forceinline__ static int column(int lq, int j, int e) { return 64 * (e / 4) + 16 * lq + 4 * j + e % 4; }
+    template <int NQ>
+    __device__ __forceinline__ void products(const Weights (&w)[NQ], f32x4 (&o)[NQ][D / 16]) const {
+#pragma unroll
+        for (int g = 0; g < D / 64; ++g)
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    o[n][4 * g] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].x, w[n][0][j], o[n][4 * g], 0, 0, 0);
+                    o[n][4 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].y, w[n][0][j], o[n][4 * g + 1], 0, 0, 0);
+                    o[n][4 * g + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].z, w[n][0][j], o[n][4 * g + 2], 0, 0, 0);
+                    o[n][4 * g + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].w, w[n][0][j], o[n][4 * g + 3], 0, 0, 0);
+                }
+            }
+    }
+};
+
+constexpr int TC_THREADS = 256, TC_WAVES = TC_THREADS / 64;
+
+// NQ: tiles of 16 queries per wavefront; QG: groups of 16 NQ queries in a block, the block's other wavefronts share the rows
+template <typename T, int D, int NQ, int QG>
+__global__ __launch_bounds__(TC_THREADS, 2) void tree_cache_kernel(TreeCall c) {
+    using Tile = CacheTile<T, D>;
+    constexpr int KT = Tile::KT, ROWS = 16 * KT, KG = TC_WAVES / QG, E = D / 16;
+    constexpr float LOG2E = 1.44269504088896341f;
+    __shared__ f32x4 s_o[2][NQ * E][64];
+    __shared__ float s_ml[2][NQ][2][64];
+    const int split = blockIdx.x, bhg = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave / KG, kg = wave % KG;
+    const int n = min(max(c.cache_len[bhg], 0), c.cap), lo = split * c.rows, last = min(n - lo, c.rows) - 1;
+    if (last < 0) return;   // uniform: the merge knows from the same length which parts exist
+    const T* K = (const T*)c.k_cache + ((size_t)bhg * c.cap + lo) * D;
+    const T* V = (const T*)c.v_cache + ((size_t)bhg * c.cap + lo) * D;
+    const T* Q = c.q_nla != nullptr ? (const T*)c.q_nla + (size_t)bhg * c.T * D : (const T*)c.q + (size_t)(bhg / c.G) * c.T * D;
+    const float scale2 = c.scale * LOG2E;
+
+    // (a tile past the end is asked for too: all its rows are the last one)
+    Tile tile;
+    int row = kg * ROWS;
+    tile.load_k(K, row, last, l16, lq);
+    tile.load_v(V, row, last, l16, lq);
+    typename Tile::Query q[NQ];
+    f32x4 o[NQ][E];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int t = (qg * NQ + i) * 16 + l16;
+        Tile::load_query(Q + (size_t)min(t, c.T - 1) * D, lq, t < c.T, q[i]);
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (; row <= last; row += KG * ROWS) {
+        const int next = row + KG * ROWS;
+        f32x4 s[NQ][KT];
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) tile.logits(q[i], s[i]);
+        tile.load_k(K, next, last, l16, lq);
+        typename Tile::Weights w[NQ];
+        const bool whole = row + ROWS - 1 <= last;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float z = s[i][t][j] * scale2;
+                    if (!whole) z = row + 16 * t + 4 * lq + j > last ? -INFINITY : z;
+                    s[i][t][j] = z;
+                    top = fmaxf(top, z);
+                }
+            top = over_quads_max(top);
+            // the running maximum follows only where a logit is more than 2^8 above it: weights stay below 2^8
+            const bool raise = top > m[i] + 8.f;   // also at the first row (m = -inf)
+            if (__any(raise)) {
+                const float corr = raise ? __builtin_amdgcn_exp2f(m[i] - top) : 1.f;
+                m[i] = raise ? top : m[i];
+                l[i] *= corr;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[i][e] *= corr;
+            }
+            const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][t][j] = __builtin_amdgcn_exp2f(s[i][t][j] - ref);
+                    l[i] += s[i][t][j];
+                }
+            Tile::weights(s[i], w[i]);
+        }
+        if (!whole) tile.clear_v(row, last, lq);
+        tile.template products<NQ>(w, o);
+        tile.load_v(V, next, last, l16, lq);
+    }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) l[i] = over_quads_sum(l[i]);
+
+    // the wavefronts that share queries: the upper half of them hands its result to the lower half, until one is left
+#pragma unroll
+    for (int half = KG / 2; half >= 1; half /= 2) {
+        const int slot = qg * half + kg % half;
+        static_assert(QG * (KG / 2) <= 2, "slots");
+        if (half < KG / 2) __syncthreads();   // the slots have been read
+        if (kg >= half && kg < 2 * half) {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                s_ml[slot][i][0][lane] = m[i];
+                s_ml[slot][i][1][lane] = l[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) s_o[slot][i * E + e][lane] = o[i][e];
+            }
+        }
+        __syncthreads();
+        if (kg < half) {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const float m2 = s_ml[slot][i][0][lane], l2 = s_ml[slot][i][1][lane];
+                const float top = fmaxf(m[i], m2), ref = top == -INFINITY ? 0.f : top;
+                const float w1 = __builtin_amdgcn_exp2f(m[i] - ref), w2 = __builtin_amdgcn_exp2f(m2 - ref);
+                m[i] = top;
+                l[i] = w1 * l[i] + w2 * l2;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[i][e] = w1 * o[i][e] + w2 * s_o[slot][i * E + e][lane];
+            }
+        }
+    }
+    if (kg != 0) return;
+    const size_t part = ((size_t)bhg * c.n_split + split) * c.T;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int t = (qg * NQ + i) * 16 + l16;
+        if (t >= c.T) continue;
+        float* out = c.ws + c.off_part + (part + t) * D;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+                *reinterpret_cast<f32x4*>(out + Tile::column(lq, j, e)) = f32x4{o[i][e][j], o[i][e + 1][j], o[i][e + 2][j], o[i][e + 3][j]};
+        if (lq == 0) *reinterpret_cast<float2*>(c.ws + c.off_ml + (part + t) * 2) = make_float2(m[i], l[i]);
+    }
+}
+
+template <typename T, int D>
+static void run_tree_cache(const TreeCall& c, hipStream_t st) {
+    const dim3 grid(c.n_split, c.B * c.H * c.G), block(TC_THREADS);
+    if (c.T <= 16) hipLaunchKernelGGL((tree_cache_kernel<T, D, 1, 1>), grid, block, 0, st, c);
+    else if (c.T <= 32) hipLaunchKernelGGL((tree_cache_kernel<T, D, 2, 1>), grid, block, 0, st, c);
+    else hipLaunchKernelGGL((tree_cache_kernel<T, D, 2, 2>), grid, block, 0, st, c);
+}
+
+// Rows of a part: as many as keep the partial results (4 T d bytes each, written and read) small beside the rows (4 d or 8 d bytes
+// each), unless there are too few parts to fill the chip.
+int tree_cache_rows(const TreeCall& c) {
+    const long long heads = (long long)c.B * c.H * c.G;
+    int rows = 1024;
+    while (rows > 128 && heads * ((c.cap + rows - 1) / rows) < 2048) rows /= 2;
+    return rows;
+}
+
+nats_status launch_tree_cache(const TreeCall& c, hipStream_t st) {
+    ProfScope ps("tree_cache", st);
+    if (c.dtype == NATS_F32) c.d == 64 ? run_tree_cache<float, 64>(c, st) : run_tree_cache<float, 128>(c, st);
+    else c.d == 64 ? run_tree_cache<bf16_t, 64>(c, st) : run_tree_cache<bf16_t, 128>(c, st);
+    return check_launch("tree_cache");
+}
+
+}  // namespace nats
