@@ -23,7 +23,7 @@ struct TreeCall {
     float* lse;
     float* ws;
     int rows, n_split;                         // rows of a part, parts of a cache
-    size_t off_ola, off_u, off_part, off_ml;   // floats
+    size_t off_ola, off_part, off_ml;   // floats
 };
 size_t tree_workspace(TreeCall& c);    // floats; fills rows, n_split and the offsets
 nats_status launch_tree(const TreeCall& c, hipStream_t st);

@@ -5,97 +5,15 @@
 #include "nats_common.h"
 #include "nats_serve.h"
 #include "serve.h"
+#include "tree_linear.h"
+#include "tree_nodes.h"
 
 namespace nats {
 
-// The ancestor set of every node as a bit mask (itself among them), by one wavefront, lane i for node i: pointer jumping, six rounds
-// whatever the tree.  parent in [-1, i - 1].
-__device__ __forceinline__ uint64_t ancestors(int parent, int lane) {
-    uint64_t m = 1ull << lane;
-    int up = parent;
-#pragma unroll
-    for (int r = 0; r < 6; ++r) {
-        const int at = up < 0 ? lane : up;
-        const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)m, at), hi = (uint32_t)__shfl((int)(uint32_t)(m >> 32), at);
-        const int next = __shfl(up, at);
-        if (up >= 0) {
-            m |= ((uint64_t)hi << 32) | lo;
-            up = next;
-        }
-    }
-    return m;
-}
-
-// parent[b][i] as the kernels use it: what is no earlier node counts as the root
-__device__ __forceinline__ int parent_of(const int32_t* parent, int b, int T, int i) {
-    const int p = i < T ? parent[(size_t)b * T + i] : -1;
-    return p >= 0 && p < i ? p : -1;
-}
-
-// ---- linear branch: a block per output head, thread r for state row r ----
-//   u_i = b_i (v_i - g_i S k_i - sum_j r_ij (k_i . k_j) u_j),  o_i = la_scale (g_i S q_i + sum_j r_ij (q_i . k_j) u_j)
-template <typename T, int D>
-__global__ __launch_bounds__(D) void tree_linear_kernel(TreeCall c) {
-    __shared__ float s_a[64], s_b[64], s_A[64][64], s_P[64][64];
-    __shared__ uint64_t s_anc[64];
-    __shared__ int s_par[64];
-    const int bhg = blockIdx.x, bh = bhg / c.G, b = bh / c.H, tid = threadIdx.x, N = c.T;
-    const T* q = (const T*)c.q + (size_t)bh * N * D;
-    const T* k = (const T*)c.k + (size_t)bh * N * D;
-    const T* v = (const T*)c.v + (size_t)bhg * N * D;
-    if (tid < 64) {
-        const int par = parent_of(c.parent, b, N, tid);
-        s_par[tid] = par;
-        s_anc[tid] = ancestors(par, tid);
-        if (tid < N) {
-            const bool soft = c.mask[(size_t)bh * N + tid] != 0;
-            s_a[tid] = soft && c.freeze ? 1.f : c.alpha[(size_t)bh * N + tid];
-            s_b[tid] = soft ? 0.f : c.beta[(size_t)bh * N + tid];
-        }
-    }
-    __syncthreads();
-    for (int e = tid; e < N * N; e += D) {
-        const int i = e / N, j = e % N;
-        if (!((s_anc[i] >> j) & 1)) continue;
-        float r = 1.f;
-        for (int n = i; n != j; n = s_par[n]) r *= s_a[n];
-        float kk = 0.f, qk = 0.f;
-        for (int x = 0; x < D; ++x) {
-            const float kj = to_float(k[j * D + x]);
-            kk += to_float(k[i * D + x]) * kj;
-            qk += to_float(q[i * D + x]) * kj;
-        }
-        s_A[i][j] = r * kk;
-        s_P[i][j] = r * qk;
-    }
-    __syncthreads();
-    float S[D];
-    for (int x = 0; x < D; ++x) S[x] = c.state[((size_t)bhg * D + tid) * D + x];
-    float* U = c.ws + c.off_u + (size_t)bhg * N * D;
-    float* O = c.ws + c.off_ola + (size_t)bhg * N * D;
-    for (int i = 0; i < N; ++i) {
-        float g = 1.f;
-        for (int n = i; n >= 0; n = s_par[n]) g *= s_a[n];
-        float sk = 0.f, sq = 0.f;
-        for (int x = 0; x < D; ++x) {
-            sk += S[x] * to_float(k[i * D + x]);
-            sq += S[x] * to_float(q[i * D + x]);
-        }
-        sk *= g;
-        sq *= g;
-        for (uint64_t m = s_anc[i] & ~(1ull << i); m; m &= m - 1) {
-            const int j = __builtin_ctzll(m);
-            if (s_b[j] == 0.f) continue;
-            sk += s_A[i][j] * U[j * D + tid];
-            sq += s_P[i][j] * U[j * D + tid];
-        }
-        if (s_b[i] != 0.f) {
-            const float u = s_b[i] * (to_float(v[i * D + tid]) - (c.linear_op == 0 ? sk : 0.f));
-            U[i * D + tid] = u;
-            sq += s_P[i][i] * u;
-        }
-        O[i * D + tid] = c.la_scale * sq;
-    }
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(TL_THREADS) void tree_linear_kernel(TreeCall c) {
+    __shared__ LinearLds<NT> s;
+    tree_linear_block<T, D, NT>(c, blockIdx.x, s);
 }
 
 // ---- the parts, the node's softmax ancestors and the linear branch's row into the output: a wavefront per node and head ----
@@ -124,8 +42,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
     }
     const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
     const uint64_t soft = __ballot(lane < N && c.mask[(size_t)bh * N + min(lane, N - 1)] != 0);
-    const uint64_t anc = ancestors(parent_of(c.parent, b, N, lane), lane);
-    const uint64_t sees = soft & (((uint64_t)(uint32_t)__shfl((int)(uint32_t)(anc >> 32), t) << 32) | (uint32_t)__shfl((int)(uint32_t)anc, t));
+    const uint64_t sees = soft & shfl_u64(ancestors(parent_of(c.parent, b, N, lane), lane), t);
     // the nodes' logits, lane j for node j, in the parts' units (powers of 2)
     constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : (const T*)c.k + (size_t)bh * N * D;
@@ -218,10 +135,8 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
     const int node = c.node[b];
     const bool refused = node < -1 || node >= N;
     if (tid < 64) {
-        const uint64_t anc = ancestors(parent_of(c.parent, b, N, tid), tid);
-        const int at = refused || node < 0 ? 0 : node;
-        const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)anc, at), hi = (uint32_t)__shfl((int)(uint32_t)(anc >> 32), at);
-        const uint64_t path = refused || node < 0 ? 0 : ((uint64_t)hi << 32) | lo;
+        const bool none = refused || node < 0;
+        const uint64_t anc = shfl_u64(ancestors(parent_of(c.parent, b, N, tid), tid), none ? 0 : node), path = none ? 0 : anc;
         const bool on = (path >> tid) & 1;
         const bool soft = on && c.mask[(size_t)bh * N + tid] != 0;
         const uint64_t softs = __ballot(soft);
@@ -285,8 +200,7 @@ size_t tree_workspace(TreeCall& c) {
     c.rows = tree_cache_rows(c);
     c.n_split = (c.cap + c.rows - 1) / c.rows;
     c.off_ola = 0;
-    c.off_u = heads * c.T * c.d;
-    c.off_part = 2 * heads * c.T * c.d;
+    c.off_part = heads * c.T * c.d;
     c.off_ml = c.off_part + heads * c.n_split * c.T * c.d;
     return c.off_ml + heads * c.n_split * c.T * 2;
 }
@@ -296,7 +210,9 @@ static nats_status run_tree(const TreeCall& c, hipStream_t st) {
     const int heads = c.B * c.H * c.G;
     {
         ProfScope ps("tree_linear", st);
-        hipLaunchKernelGGL((tree_linear_kernel<T, D>), dim3(heads), dim3(D), 0, st, c);
+        if (c.T <= 16) hipLaunchKernelGGL((tree_linear_kernel<T, D, 1>), dim3(heads), dim3(TL_THREADS), 0, st, c);
+        else if (c.T <= 32) hipLaunchKernelGGL((tree_linear_kernel<T, D, 2>), dim3(heads), dim3(TL_THREADS), 0, st, c);
+        else hipLaunchKernelGGL((tree_linear_kernel<T, D, 4>), dim3(heads), dim3(TL_THREADS), 0, st, c);
     }
     const nats_status r = launch_tree_cache(c, st);
     if (r != NATS_OK) return r;

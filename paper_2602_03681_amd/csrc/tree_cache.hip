@@ -20,14 +20,10 @@
 #include "mfma_util.h"
 #include "nats_common.h"
 #include "serve.h"
+#include "softmax_terms.h"
 
 namespace nats {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
 // over the lanes l, l ^ 16, l ^ 32, l ^ 48, which share a query
 __device__ __forceinline__ float over_quads_max(float x) {
     const int lane = threadIdx.x & 63;
@@ -198,7 +194,8 @@ __global__ __launch_bounds__(TC_THREADS, 2) void tree_cache_kernel(TreeCall c) {
     const T* Q = c.q_nla != nullptr ? (const T*)c.q_nla + (size_t)bhg * c.T * D : (const T*)c.q + (size_t)(bhg / c.G) * c.T * D;
     const float scale2 = c.scale * LOG2E;
 
-    // (a tile past the end is asked for too: all its rows are the last one)
+    // (A tile past the end is asked for too, all its rows the last one: with the loads behind a condition the compiler gave registers of
+    // the V tile to temporaries.)
     Tile tile;
     int row = kg * ROWS;
     tile.load_k(K, row, last, l16, lq);

@@ -1,0 +1,250 @@
+// Linear branch of a tree of drafted tokens (internal header): the work of a block of four wavefronts for one output head.
+//
+// With a_i the decay and b_i the write strength of node i, g_i the product of the decays on its path and r_ij that of the decays behind
+// ancestor j up to i, the states of all nodes are sums over their ancestors, and S itself is read once:
+//   S_i = g_i S + sum_j r_ij u_j k_j^T                              (j: ancestors of i and i)
+//   u_i = b_i (v_i - g_i S k_i + sum_{j != i} n_ij u_j / b_i),      n_ij = -b_i r_ij (k_i . k_j)
+//   o_i = la_scale (g_i S q_i + sum_j r_ij (q_i . k_j) u_j)
+// i.e. (I - N) U = diag(b) (V - diag(g) K S^T) with N strictly lower triangular, since parents come first.  It is solved by blocks of
+// 16 nodes, the diagonal blocks' inverses made once per head.
+//
+// A wavefront takes 16 rows of S (columns of U) at a time and needs nothing of the others': K S^T, the solution and P U are products whose
+// result tiles are the next one's operand as they sit in registers.  K S^T and Q S^T run on the bf16 instruction with S as three bf16
+// terms (all of its bits), the products with N, P and U, up to 64 x 64, on the fp32 one.
+//
+// In a product a node that is no ancestor has a coefficient of 0, which an infinity or a NaN in its u turns into NaN.  So a wavefront
+// whose u are not all finite does its columns again, ancestor by ancestor.
+#pragma once
+#include "nats_common.h"
+#include "serve.h"
+#include "softmax_terms.h"
+#include "tree_nodes.h"
+
+namespace nats {
+
+constexpr int TL_THREADS = 256, TL_WAVES = TL_THREADS / 64;
+
+template <int NT>   // tiles of 16 nodes
+struct LinearLds {
+    static constexpr int N = 16 * NT;
+    float n[N][N + 4], p[N][N + 4];      // rows of fp32 operands: 16-byte reads of 16 rows
+    float inv[NT][16][20];
+    float u[TL_WAVES][N][16];
+    float a[64], b[64], g[64];
+    double lg[64];                       // log2 g
+    uint64_t anc[64];
+    int par[64];
+    int plain;                           // every decay is an ordinary positive number
+};
+
+__device__ __forceinline__ float4 as_float4(f32x4 x) { return make_float4(x[0], x[1], x[2], x[3]); }
+
+template <typename T, int D, int NT>
+__device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, LinearLds<NT>& s) {
+    constexpr int KS = D / 32;
+    const int bh = bhg / c.G, b = bh / c.H, N = c.T, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const T* q = (const T*)c.q + (size_t)bh * N * D;
+    const T* k = (const T*)c.k + (size_t)bh * N * D;
+    const T* v = (const T*)c.v + (size_t)bhg * N * D;
+    const float* S = c.state + (size_t)bhg * D * D;
+
+    // the first rows of S are on their way while the tree is looked at
+    Raw8<float> sr[KS];
+    auto load_state = [&](int row0) {
+#pragma unroll
+        for (int i = 0; i < KS; ++i) sr[i].load(S + (size_t)(row0 + l16) * D + 32 * i + 8 * lq);
+    };
+    load_state(16 * wave);
+
+    // ---- paths, their decays ----
+    if (wave == 0) {
+        const int there = c.n_nodes != nullptr ? min(c.n_nodes[b], N) : N, par = parent_of(c.parent, b, N, lane);
+        const bool soft = c.mask[(size_t)bh * N + min(lane, N - 1)] != 0;
+        float a = c.alpha[(size_t)bh * N + min(lane, N - 1)], bt = c.beta[(size_t)bh * N + min(lane, N - 1)];
+        if (lane >= N || (soft && c.freeze)) a = 1.f;
+        if (lane >= there || soft) bt = 0.f;
+        float g = a;
+        double lg = log2((double)a);
+        along_paths(par, lane, [&](bool up, int from) {
+            const float more = __shfl(g, from);
+            const uint64_t l = shfl_u64(__double_as_longlong(lg), from);
+            if (up) {
+                g *= more;
+                lg += __longlong_as_double(l);
+            }
+        });
+        const bool plain = __all(a > 0x1p-120f && a < 0x1p120f);
+        s.anc[lane] = ancestors(par, lane);
+        s.par[lane] = par;
+        s.a[lane] = a;
+        s.b[lane] = bt;
+        s.g[lane] = g;
+        s.lg[lane] = lg;
+        if (lane == 0) s.plain = plain;
+    }
+
+    // ---- N and P: the lower triangle's tiles, dealt out to the wavefronts ----
+    auto load_nodes = [&](const T* x, int tile, Raw8<T> (&r)[KS]) {
+        const T* p = x + (size_t)min(16 * tile + l16, N - 1) * D + 8 * lq;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) r[i].load(p + 32 * i);
+    };
+    constexpr int PAIRS = NT * (NT + 1) / 2, PER_WAVE = (PAIRS + TL_WAVES - 1) / TL_WAVES;
+    f32x4 kk[PER_WAVE], qk[PER_WAVE];
+#pragma unroll
+    for (int x = 0; x < PER_WAVE; ++x) {
+        const int pair = wave + x * TL_WAVES;
+        if (pair >= PAIRS) break;
+        const int ti = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, tj = pair - ti * (ti + 1) / 2;
+        kk[x] = qk[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (16 * ti >= N) continue;
+        Raw8<T> ki[KS], qi[KS], kj[KS];
+        load_nodes(k, ti, ki);
+        load_nodes(q, ti, qi);
+        load_nodes(k, tj, kj);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            u32x4 tk[terms_of<T>()], tq[terms_of<T>()], tb[terms_of<T>()];
+            ki[i].terms(tk);
+            qi[i].terms(tq);
+            kj[i].terms(tb);
+            kk[x] = mfma_terms(tk, tb, kk[x]);
+            qk[x] = mfma_terms(tq, tb, qk[x]);
+        }
+    }
+    __syncthreads();
+    const bool plain = s.plain != 0;
+#pragma unroll
+    for (int x = 0; x < PER_WAVE; ++x) {
+        const int pair = wave + x * TL_WAVES;
+        if (pair >= PAIRS) break;
+        const int ti = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, tj = pair - ti * (ti + 1) / 2;
+        const int j = 16 * tj + l16;
+        const double lgj = s.lg[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 16 * ti + 4 * lq + e;
+            const bool on = (s.anc[i] >> j) & 1;
+            float r = 0.f;
+            if (plain) {
+                r = __builtin_amdgcn_exp2f((float)(s.lg[i] - lgj));
+            } else if (on) {
+                r = 1.f;
+                for (int m = i; m != j; m = s.par[m]) r *= s.a[m];
+            }
+            s.n[i][j] = on && i != j ? -s.b[i] * r * kk[x][e] : 0.f;
+            s.p[i][j] = on ? r * qk[x][e] : 0.f;
+        }
+    }
+    __syncthreads();
+    // ---- the diagonal blocks' inverses: lane (tile, column) ----
+    if (wave == 0 && lane < 16 * NT && c.linear_op == 0) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float sum = i == l16 ? 1.f : 0.f;
+#pragma unroll
+            for (int j = 0; j < i; ++j) sum += s.n[16 * lq + i][16 * lq + j] * x[j];
+            x[i] = sum;
+            s.inv[lq][i][l16] = sum;
+        }
+    }
+    __syncthreads();
+
+    // ---- 16 columns at a time ----
+    float* O = c.ws + c.off_ola + (size_t)bhg * N * D;
+#pragma unroll
+    for (int turn = 0; turn < D / (16 * TL_WAVES); ++turn) {
+        const int col = 16 * (turn * TL_WAVES + wave) + l16;
+        f32x4 w[NT], o[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            u32x4 ts[N_TERMS];
+            sr[i].terms(ts);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                Raw8<T> x;
+                u32x4 tx[terms_of<T>()];
+                const size_t at = (size_t)min(16 * t + l16, N - 1) * D + 32 * i + 8 * lq;
+                x.load(k + at);
+                x.terms(tx);
+                w[t] = mfma_terms(tx, ts, w[t]);
+                x.load(q + at);
+                x.terms(tx);
+                o[t] = mfma_terms(tx, ts, o[t]);
+            }
+        }
+        if (turn + 1 < D / (16 * TL_WAVES)) load_state(16 * ((turn + 1) * TL_WAVES + wave));
+        f32x4 u[NT];
+        bool fine = true;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const f32x4 g = *reinterpret_cast<const f32x4*>(&s.g[16 * t + 4 * lq]), bt = *reinterpret_cast<const f32x4*>(&s.b[16 * t + 4 * lq]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = to_float(v[(size_t)min(16 * t + 4 * lq + e, N - 1) * D + col]);
+                w[t][e] = bt[e] == 0.f ? 0.f : bt[e] * (c.linear_op == 0 ? x - g[e] * w[t][e] : x);
+                o[t][e] *= g[e];
+            }
+            u[t] = w[t];
+            if (c.linear_op == 0) {
+#pragma unroll
+                for (int x = 0; x < t; ++x) u[t] = mac16(ld4(&s.n[16 * t + l16][16 * x + 4 * lq]), as_float4(u[x]), u[t]);
+                u[t] = mac16(ld4(&s.inv[t][l16][4 * lq]), as_float4(u[t]), f32x4{0.f, 0.f, 0.f, 0.f});
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) fine = fine && fabsf(u[t][e]) < INFINITY;
+        }
+        if (__all(fine)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int x = 0; x <= t; ++x) o[t] = mac16(ld4(&s.p[16 * t + l16][16 * x + 4 * lq]), as_float4(u[x]), o[t]);
+        } else {
+            // ancestor by ancestor: 16 lanes a column each for u, then every lane its results
+            float(&su)[16 * NT][16] = s.u[wave];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) su[16 * t + 4 * lq + e][l16] = w[t][e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+            if (lq == 0 && c.linear_op == 0) {
+                for (int i = 0; i < N; ++i) {
+                    float sum = su[i][l16];
+                    if (s.b[i] == 0.f) continue;
+                    for (uint64_t m = s.anc[i] & ~(1ull << i); m; m &= m - 1) {
+                        const int j = __builtin_ctzll(m);
+                        if (s.b[j] != 0.f) sum += s.n[i][j] * su[j][l16];
+                    }
+                    su[i][l16] = sum;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 16 * t + 4 * lq + e;
+                    for (uint64_t m = i < N ? s.anc[i] : 0; m; m &= m - 1) {
+                        const int j = __builtin_ctzll(m);
+                        if (s.b[j] != 0.f) o[t][e] += s.p[i][j] * su[j][l16];
+                    }
+                }
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * t + 4 * lq + e;
+                if (i < N) O[(size_t)i * D + col] = c.la_scale * o[t][e];
+            }
+    }
+}
+
+}  // namespace nats
