@@ -27,7 +27,7 @@ typedef struct nats_tree_params {
     int32_t B, H;          /* sequences, linear heads                                                */
     int32_t T;             /* drafted tokens (nodes) per sequence, 1 .. NATS_TREE_MAX_NODES           */
     int32_t d;             /* 64 or 128                                                               */
-    int32_t cap;           /* rows per (b, head) in the KV cache                                      */
+    int32_t cap;           /* rows per (b, head) in the KV cache, at most 2^20 (in all the calls here)  */
     int32_t dtype;         /* nats_dtype of q, k, v, o and of the KV cache                            */
     float softmax_scale;   /* as in nats_dec_params                                                   */
     float la_scale;
@@ -77,7 +77,7 @@ nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state
 
 typedef struct nats_cache_weights_params {
     int32_t B, H;          /* sequences, heads of the cache (all output heads)                         */
-    int32_t T;             /* queries per (b, head)                                                   */
+    int32_t T;             /* queries per (b, head), at most 2^20                                      */
     int32_t d, cap, dtype; /* as above                                                                */
     int32_t q_group;       /* q is [B,H/q_group,T,d]: a query head serves q_group heads in a row (0 counts as 1) */
     int32_t vis_group;     /* vis is [B,H/vis_group,T]                                                */

@@ -4,9 +4,58 @@
 #include "nats_common.h"
 #include "nats_serve.h"
 #include "serve.h"
+#include "softmax_terms.h"
 
 namespace nats {
 
+// ---- attention weights of a cache's rows ----------------------------------------------------------------------------------
+//   w[c] <- decay w[c] + sum_t [c < vis_t] exp2(s q_t . k_c - L_t),   s = scale log2(e), L_t = lse_t log2(e)
+// A product of queries and rows whose result is summed over the queries: with the rows as columns of a result tile a lane keeps one sum per
+// row.  Few queries (a step's): the queries stay in registers and the rows of K stream, memory-bound.  Many (a prompt's): 16 or more rows
+// stay and the queries stream; bound by the exponential, four cycles a piece per lane and pair, beside the same of matrix instructions.
+//
+// Without lse the sums over the cache are needed first.  Up to 16 queries the first pass then keeps its logits, 4 T bytes a row
+// where K has 2 d or 4 d, and K is read once; beyond, writing and reading them would cost as much as K again.
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr int CW_THREADS = 256, CW_WAVES = CW_THREADS / 64;
+constexpr int CW_FEW = 64;       // queries that stay in registers
+constexpr int CW_KEEP = 16;      // queries whose logits are kept
+
+// 16 rows of D elements as an operand (lane l16: row, lane quarter lq: its share of every 32 or 16 columns), and the product of two
+template <typename T, int D>
+struct Rows16;
+template <int D>
+struct Rows16<bf16_t, D> {
+    u32x4 x[D / 32];
+    __device__ __forceinline__ void load(const bf16_t* p, int row, int last, int l16, int lq) {
+        p += (size_t)min(row + l16, last) * D + 8 * lq;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
+    }
+    __device__ __forceinline__ static f32x4 product(const Rows16& a, const Rows16& b) {
+        f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) s = mfma_bf16(a.x[i], b.x[i], s);
+        return s;
+    }
+};
+template <int D>
+struct Rows16<float, D> {
+    float4 x[D / 16];
+    __device__ __forceinline__ void load(const float* p, int row, int last, int l16, int lq) {
+        p += (size_t)min(row + l16, last) * D + 4 * lq;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) x[i] = ld4(p + 16 * i);
+    }
+    __device__ __forceinline__ static f32x4 product(const Rows16& a, const Rows16& b) {
+        f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) s = mac16(a.x[i], b.x[i], s);
+        return s;
+    }
+};
+
+__device__ __forceinline__ int rows_of(const WeightsCall& c, int bh) { return min(max(c.cache_len[bh], 0), c.cap); }
 // rows of the cache that query t of head bh sees
 __device__ __forceinline__ int sees_rows(const WeightsCall& c, int bh, int t, int n) {
     if (c.vis == nullptr) return n;
@@ -14,75 +63,360 @@ __device__ __forceinline__ int sees_rows(const WeightsCall& c, int bh, int t, in
     return min(max(c.vis[((size_t)b * (c.H / c.vis_group) + h / c.vis_group) * c.T + t], 0), n);
 }
 template <typename T>
-__device__ __forceinline__ const T* query(const WeightsCall& c, int bh, int t) {
+__device__ __forceinline__ const T* queries(const WeightsCall& c, int bh) {
     const int b = bh / c.H, h = bh % c.H;
-    return (const T*)c.q + (((size_t)b * (c.H / c.q_group) + h / c.q_group) * c.T + t) * c.d;
+    return (const T*)c.q + ((size_t)b * (c.H / c.q_group) + h / c.q_group) * c.T * c.d;
+}
+// running maximum and sum of two parts into one
+__device__ __forceinline__ void join(float& m, float& l, float m2, float l2) {
+    const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+    l = l * __builtin_amdgcn_exp2f(m - ref) + l2 * __builtin_amdgcn_exp2f(m2 - ref);
+    m = top;
 }
 
-// ---- log-sum-exp of the rows a query sees: a block per query ----
-constexpr int CW_THREADS = 256;
-template <typename T, int D>
+// ---- first pass without lse: maximum and sum of up to 16 NQ queries over a part of the rows; KEEP: the logits, too ----
+// Result tiles have the rows of K as rows: a lane has 4 rows in a row of one query.
+template <typename T, int D, int NQ, bool KEEP>
+__global__ __launch_bounds__(CW_THREADS, 2) void weights_sums_kernel(WeightsCall c) {
+    constexpr int KT = 2;   // tiles of rows in flight
+    __shared__ float2 s_ml[CW_WAVES][NQ][16];
+    const int bh = blockIdx.x, part = blockIdx.y, t0 = blockIdx.z * 16 * NQ, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = rows_of(c, bh), lo = part * c.rows, last = min(n - lo, c.rows) - 1;
+    if (last < 0) return;
+    const T* K = (const T*)c.k_cache + ((size_t)bh * c.cap + lo) * D;
+    Rows16<T, D> q[NQ], k[KT];
+    int row = wave * 16 * KT;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) k[i].load(K, row + 16 * i, last, l16, lq);
+    int vis[NQ];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int t = min(t0 + 16 * x + l16, c.T - 1);
+        q[x].load(queries<T>(c, bh), t0 + 16 * x, c.T - 1, l16, lq);
+        vis[x] = sees_rows(c, bh, t, n) - lo;
+        m[x] = -INFINITY;
+        l[x] = 0.f;
+    }
+    const float scale2 = c.scale * LOG2E;
+    for (; row <= last; row += CW_WAVES * 16 * KT) {
+        f32x4 s[NQ][KT];
+#pragma unroll
+        for (int i = 0; i < KT; ++i)
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) s[x][i] = Rows16<T, D>::product(k[i], q[x]);
+#pragma unroll
+        for (int i = 0; i < KT; ++i) k[i].load(K, row + CW_WAVES * 16 * KT + 16 * i, last, l16, lq);
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            float top = m[x];
+#pragma unroll
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = row + 16 * i + 4 * lq + j;
+                    s[x][i][j] = r <= last && r < vis[x] ? s[x][i][j] * scale2 : -INFINITY;
+                    top = fmaxf(top, s[x][i][j]);
+                }
+            const float ref = top == -INFINITY ? 0.f : top;
+            l[x] *= __builtin_amdgcn_exp2f(m[x] - ref);
+            m[x] = top;
+#pragma unroll
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) l[x] += __builtin_amdgcn_exp2f(s[x][i][j] - ref);
+            if (KEEP && l16 < c.T) {
+#pragma unroll
+                for (int i = 0; i < KT; ++i)   // (rows past the end within the part have their place, too)
+                    if (row + 16 * i + 4 * lq <= last)
+                        *reinterpret_cast<f32x4*>(c.ws + c.off_logits + ((size_t)bh * c.T + l16) * c.pitch + lo + row + 16 * i + 4 * lq) = s[x][i];
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        join(m[x], l[x], lane_xor16(m[x], lane), lane_xor16(l[x], lane));
+        join(m[x], l[x], lane_xor32(m[x], lane), lane_xor32(l[x], lane));
+        if (lq == 0) s_ml[wave][x][l16] = make_float2(m[x], l[x]);
+    }
+    __syncthreads();
+    const int t = t0 + (int)threadIdx.x;
+    if (threadIdx.x >= 16 * NQ || t >= c.T) return;
+    float2 r = s_ml[0][threadIdx.x / 16][threadIdx.x % 16];
+#pragma unroll
+    for (int w = 1; w < CW_WAVES; ++w) join(r.x, r.y, s_ml[w][threadIdx.x / 16][threadIdx.x % 16].x, s_ml[w][threadIdx.x / 16][threadIdx.x % 16].y);
+    *reinterpret_cast<float2*>(c.ws + c.off_ml + (((size_t)bh * c.parts + part) * c.T + t) * 2) = r;
+}
+
+// the parts' maxima and sums into the log-sum-exp, a thread per query
 __global__ __launch_bounds__(CW_THREADS) void weights_lse_kernel(WeightsCall c) {
-    __shared__ float s_q[D], s_m[4], s_l[4];
-    const int t = blockIdx.x, bh = blockIdx.y, tid = threadIdx.x;
-    const int n = min(max(c.cache_len[bh], 0), c.cap), vis = sees_rows(c, bh, t, n);
-    if (tid < D) s_q[tid] = to_float(query<T>(c, bh, t)[tid]) * c.scale;
-    __syncthreads();
-    const T* K = (const T*)c.k_cache + (size_t)bh * c.cap * D;
+    const int bh = blockIdx.x, t = blockIdx.y * CW_THREADS + threadIdx.x;
+    if (t >= c.T) return;
+    const int parts = (rows_of(c, bh) + c.rows - 1) / c.rows;
     float m = -INFINITY, l = 0.f;
-    for (int r = tid; r < vis; r += CW_THREADS) {
-        float x = 0.f;
-        for (int e = 0; e < D; ++e) x += s_q[e] * to_float(K[(size_t)r * D + e]);
-        const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top;
-        l = l * expf(m - ref) + expf(x - ref);
-        m = top;
+    for (int p = 0; p < parts; ++p) {
+        const float2 x = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (((size_t)bh * c.parts + p) * c.T + t) * 2);
+        join(m, l, x.x, x.y);
     }
-    float top = m;
-    for (int w = 1; w < 64; w *= 2) top = fmaxf(top, __shfl_xor(top, w));
-    l = lane_group_sum<64>(l * expf(m - (top == -INFINITY ? 0.f : top)));
-    if ((tid & 63) == 0) { s_m[tid >> 6] = top; s_l[tid >> 6] = l; }
+    c.ws[c.off_lse + (size_t)bh * c.T + t] = l == 0.f ? -INFINITY : (m + log2f(l)) / LOG2E;
+}
+
+// ---- the weights from logits that were kept: a thread per row ----
+__global__ __launch_bounds__(CW_THREADS) void weights_kept_kernel(WeightsCall c) {
+    __shared__ float s_m[CW_THREADS], s_l[CW_THREADS], s_lse[CW_KEEP];
+    const int bh = blockIdx.x, tid = threadIdx.x, r = blockIdx.y * CW_THREADS + tid, n = rows_of(c, bh);
+    if ((int)blockIdx.y * CW_THREADS >= n) return;
+    const float* z = c.ws + c.off_logits + (size_t)bh * c.T * c.pitch + r;
+    float x[CW_KEEP], w = 0.f;
+#pragma unroll
+    for (int t = 0; t < CW_KEEP; ++t) x[t] = t < c.T && r < n ? z[(size_t)t * c.pitch] : -INFINITY;
+    if (r < n) w = c.decay * c.weights[(size_t)bh * c.cap + r];
+    {   // the parts of query tid % 16, sixteen threads to a query
+        const int t = tid % CW_KEEP, parts = (n + c.rows - 1) / c.rows;
+        float m = -INFINITY, l = 0.f;
+        for (int p = tid / CW_KEEP; t < c.T && p < parts; p += CW_THREADS / CW_KEEP) {
+            const float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (((size_t)bh * c.parts + p) * c.T + t) * 2);
+            join(m, l, ml.x, ml.y);
+        }
+        s_m[tid] = m;
+        s_l[tid] = l;
+    }
     __syncthreads();
-    if (tid == 0) {
-        float M = s_m[0], L = 0.f;
-        for (int i = 1; i < 4; ++i) M = fmaxf(M, s_m[i]);
-        for (int i = 0; i < 4; ++i) L += s_l[i] * expf(s_m[i] - (M == -INFINITY ? 0.f : M));
-        c.ws[(size_t)bh * c.T + t] = vis > 0 ? M + logf(L) : -INFINITY;
+    if (tid < CW_KEEP) {
+        float m = s_m[tid], l = s_l[tid];
+        for (int i = 1; i < CW_THREADS / CW_KEEP; ++i) join(m, l, s_m[i * CW_KEEP + tid], s_l[i * CW_KEEP + tid]);
+        s_lse[tid] = l == 0.f ? INFINITY : m + log2f(l);   // a query that sees nothing: all its logits are -inf
     }
-}
-
-// ---- the weights: a thread per row ----
-template <typename T, int D>
-__global__ __launch_bounds__(CW_THREADS) void weights_add_kernel(WeightsCall c) {
-    const int bh = blockIdx.y, r = blockIdx.x * CW_THREADS + threadIdx.x;
-    const int n = min(max(c.cache_len[bh], 0), c.cap);
+    __syncthreads();
     if (r >= n) return;
-    const T* K = (const T*)c.k_cache + ((size_t)bh * c.cap + r) * D;
-    const float* lse = (c.lse != nullptr ? c.lse : c.ws) + (size_t)bh * c.T;
-    float k[D];
-    for (int e = 0; e < D; ++e) k[e] = to_float(K[e]) * c.scale;
     float sum = 0.f;
-    for (int t = 0; t < c.T; ++t) {
-        if (r >= sees_rows(c, bh, t, n) || lse[t] == -INFINITY) continue;
-        const T* q = query<T>(c, bh, t);
-        float x = 0.f;
-        for (int e = 0; e < D; ++e) x += to_float(q[e]) * k[e];
-        sum += expf(x - lse[t]);
-    }
-    float* w = c.weights + (size_t)bh * c.cap + r;
-    *w = c.decay * *w + sum;
+#pragma unroll
+    for (int t = 0; t < CW_KEEP; ++t)
+        if (t < c.T) sum += __builtin_amdgcn_exp2f(x[t] - s_lse[t]);
+    c.weights[(size_t)bh * c.cap + r] = w + sum;
 }
 
-size_t weights_workspace(const WeightsCall& c, bool lse_given) { return lse_given ? 0 : (size_t)c.B * c.H * c.T; }
+// lse in powers of two and the number of visible rows of queries t .. t + 3 (those beyond T see nothing, nor do those with lse -inf)
+__device__ __forceinline__ void query_bounds(const WeightsCall& c, const float* lse, int bh, int t, int n, f32x4& L, int (&vis)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int at = min(t + j, c.T - 1);
+        const float x = lse[at];
+        L[j] = x * LOG2E;
+        vis[j] = t + j < c.T && x != -INFINITY ? sees_rows(c, bh, at, n) : 0;
+    }
+}
+
+// ---- few queries: they stay, the rows stream ----
+template <typename T, int D, int NQ>
+__global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall c) {
+    constexpr int KT = sizeof(T) == 4 && D == 128 && NQ == 4 ? 1 : 2;   // (two would not fit into the registers)
+    const int bh = blockIdx.x, part = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = rows_of(c, bh), lo = part * c.rows, last = min(n - lo, c.rows) - 1;
+    if (last < 0) return;
+    const T* K = (const T*)c.k_cache + ((size_t)bh * c.cap + lo) * D;
+    const float* lse = (c.lse != nullptr ? c.lse : c.ws + c.off_lse) + (size_t)bh * c.T;
+    float* weights = c.weights + (size_t)bh * c.cap + lo;
+    Rows16<T, D> q[NQ], k[KT];
+    int row = wave * 16 * KT;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) k[i].load(K, row + 16 * i, last, l16, lq);
+    f32x4 L[NQ];
+    int vis[NQ][4];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        q[x].load(queries<T>(c, bh), 16 * x, c.T - 1, l16, lq);
+        query_bounds(c, lse, bh, 16 * x + 4 * lq, n, L[x], vis[x]);
+    }
+    const float scale2 = c.scale * LOG2E;
+    for (; row <= last; row += CW_WAVES * 16 * KT) {
+        float sum[KT], w[KT];
+        f32x4 s[KT][NQ];
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+            w[i] = weights[min(row + 16 * i + l16, last)];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) s[i][x] = Rows16<T, D>::product(q[x], k[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < KT; ++i) k[i].load(K, row + CW_WAVES * 16 * KT + 16 * i, last, l16, lq);
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+            const int r = row + 16 * i + l16;
+            sum[i] = 0.f;
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(s[i][x][j] * scale2 - L[x][j]);
+                    sum[i] += lo + r < vis[x][j] ? p : 0.f;
+                }
+            sum[i] += lane_xor16(sum[i], lane);
+            sum[i] += lane_xor32(sum[i], lane);
+            if (lq == 0 && r <= last) weights[r] = c.decay * w[i] + sum[i];
+        }
+    }
+}
+
+// ---- many queries: 16 KT rows stay in every wavefront's registers, the block's wavefronts share its queries ----
+template <typename T, int D>
+constexpr int many_tiles() { return sizeof(T) == 2 || D == 64 ? 4 : 2; }
+
+template <typename T, int D>
+__global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall c) {
+    constexpr int KT = many_tiles<T, D>();
+    __shared__ float s_sum[CW_WAVES][16 * KT];
+    const int bh = blockIdx.x, r0 = blockIdx.y * 16 * KT, split = blockIdx.z, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = rows_of(c, bh);
+    if (r0 >= n) return;
+    const T* Q = queries<T>(c, bh);
+    const float* lse = (c.lse != nullptr ? c.lse : c.ws + c.off_lse) + (size_t)bh * c.T;
+    const float scale2 = c.scale * LOG2E;
+    const int end = min((split + 1) * c.chunk, c.T);
+    Rows16<T, D> k[KT], q;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) k[i].load((const T*)c.k_cache + (size_t)bh * c.cap * D, r0 + 16 * i, n - 1, l16, lq);
+    float sum[KT];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) sum[i] = 0.f;
+    int t = split * c.chunk + 16 * wave;
+    f32x4 L, nextL;
+    int vis[4], next_vis[4];
+    q.load(Q, t, c.T - 1, l16, lq);
+    query_bounds(c, lse, bh, t + 4 * lq, n, L, vis);
+    for (; t < end; t += 16 * CW_WAVES) {
+        const int least = min(min(vis[0], vis[1]), min(vis[2], vis[3])), most = max(max(vis[0], vis[1]), max(vis[2], vis[3]));
+        const bool any = __any(most > r0), all = __all(least >= r0 + 16 * KT);
+        f32x4 s[KT];
+        if (any) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i) s[i] = Rows16<T, D>::product(q, k[i]);
+        }
+        q.load(Q, t + 16 * CW_WAVES, c.T - 1, l16, lq);
+        query_bounds(c, lse, bh, t + 16 * CW_WAVES + 4 * lq, n, nextL, next_vis);
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[i] += __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
+        } else if (any) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p = __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
+                    sum[i] += r0 + 16 * i + l16 < vis[j] ? p : 0.f;
+                }
+        }
+        L = nextL;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vis[j] = next_vis[j];
+    }
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+        sum[i] += lane_xor16(sum[i], lane);
+        sum[i] += lane_xor32(sum[i], lane);
+        if (lq == 0) s_sum[wave][16 * i + l16] = sum[i];
+    }
+    __syncthreads();
+    const int r = r0 + (int)threadIdx.x;
+    if (threadIdx.x >= 16 * KT || r >= n) return;
+    float x = s_sum[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < CW_WAVES; ++w) x += s_sum[w][threadIdx.x];
+    c.ws[c.off_sums + ((size_t)split * c.B * c.H + bh) * c.cap + r] = x;
+}
+
+// the splits' sums onto the weights, in order
+__global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c) {
+    const int bh = blockIdx.x, r = blockIdx.y * CW_THREADS + threadIdx.x;
+    if (r >= rows_of(c, bh)) return;
+    float x = 0.f;
+    for (int s = 0; s < c.splits; ++s) x += c.ws[c.off_sums + ((size_t)s * c.B * c.H + bh) * c.cap + r];
+    float* w = c.weights + (size_t)bh * c.cap + r;
+    *w = c.decay * *w + x;
+}
+
+// Rows of a part: enough parts to fill the chip, where there are rows for that.
+size_t weights_workspace(WeightsCall& c, bool lse_given) {
+    const long long heads = (long long)c.B * c.H;
+    c.rows = 1024;
+    while (c.rows > 128 && heads * ((c.cap + c.rows - 1) / c.rows) < 2048) c.rows /= 2;
+    c.parts = (c.cap + c.rows - 1) / c.rows;
+    size_t at = 0;
+    if (!lse_given) {
+        c.off_ml = at;
+        at += (size_t)heads * c.parts * c.T * 2;
+        at = align_up(at, 4);
+        if (c.T <= CW_KEEP) {
+            c.pitch = (c.cap + 31) / 32 * 32;
+            c.off_logits = at;
+            at += (size_t)heads * c.T * c.pitch;
+        } else {
+            c.off_lse = at;
+            at += (size_t)heads * c.T;
+        }
+    }
+    if (c.T > CW_FEW) {
+        // queries per block: as many as leave enough blocks
+        const int tiles = 16 * (c.dtype == NATS_BF16 || c.d == 64 ? 4 : 2);
+        const long long blocks = heads * ((c.cap + tiles - 1) / tiles);
+        c.chunk = 2048;
+        while (c.chunk > 128 && blocks * ((c.T + c.chunk - 1) / c.chunk) < 2048) c.chunk /= 2;
+        c.splits = (c.T + c.chunk - 1) / c.chunk;
+        c.off_sums = at;
+        at += (size_t)c.splits * heads * c.cap;
+    }
+    return at;
+}
+
+template <typename T, int D>
+static void run_sums(const WeightsCall& c, hipStream_t st) {
+    const int heads = c.B * c.H;
+    const dim3 block(CW_THREADS);
+    if (c.T <= CW_KEEP) {
+        hipLaunchKernelGGL((weights_sums_kernel<T, D, 1, true>), dim3(heads, c.parts), block, 0, st, c);
+    } else if (c.T <= 32) {
+        hipLaunchKernelGGL((weights_sums_kernel<T, D, 2, false>), dim3(heads, c.parts), block, 0, st, c);
+    } else {
+        hipLaunchKernelGGL((weights_sums_kernel<T, D, 4, false>), dim3(heads, c.parts, (c.T + 63) / 64), block, 0, st, c);
+    }
+}
 
 template <typename T, int D>
 static nats_status run_weights(const WeightsCall& c, hipStream_t st) {
     const int heads = c.B * c.H;
+    const dim3 block(CW_THREADS), rows(heads, (c.cap + CW_THREADS - 1) / CW_THREADS);
     if (c.lse == nullptr) {
-        ProfScope ps("cache_weights_lse", st);
-        hipLaunchKernelGGL((weights_lse_kernel<T, D>), dim3(c.T, heads), dim3(CW_THREADS), 0, st, c);
+        {
+            ProfScope ps("weights_sums", st);
+            run_sums<T, D>(c, st);
+        }
+        if (c.T <= CW_KEEP) {
+            ProfScope ps("weights_kept", st);
+            hipLaunchKernelGGL(weights_kept_kernel, rows, block, 0, st, c);
+            return check_launch("cache_weights");
+        }
+        ProfScope ps("weights_lse", st);
+        hipLaunchKernelGGL(weights_lse_kernel, dim3(heads, (c.T + CW_THREADS - 1) / CW_THREADS), block, 0, st, c);
     }
-    ProfScope ps("cache_weights", st);
-    hipLaunchKernelGGL((weights_add_kernel<T, D>), dim3((c.cap + CW_THREADS - 1) / CW_THREADS, heads), dim3(CW_THREADS), 0, st, c);
+    if (c.T <= CW_FEW) {
+        ProfScope ps("weights_few", st);
+        if (c.T <= 16) hipLaunchKernelGGL((weights_few_kernel<T, D, 1>), dim3(heads, c.parts), block, 0, st, c);
+        else if (c.T <= 32) hipLaunchKernelGGL((weights_few_kernel<T, D, 2>), dim3(heads, c.parts), block, 0, st, c);
+        else hipLaunchKernelGGL((weights_few_kernel<T, D, 4>), dim3(heads, c.parts), block, 0, st, c);
+        return check_launch("cache_weights");
+    }
+    {
+        ProfScope ps("weights_many", st);
+        constexpr int ROWS = 16 * many_tiles<T, D>();
+        hipLaunchKernelGGL((weights_many_kernel<T, D>), dim3(heads, (c.cap + ROWS - 1) / ROWS, c.splits), block, 0, st, c);
+    }
+    ProfScope ps("weights_join", st);
+    hipLaunchKernelGGL(weights_join_kernel, rows, block, 0, st, c);
     return check_launch("cache_weights");
 }
 

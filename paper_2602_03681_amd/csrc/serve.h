@@ -52,8 +52,12 @@ struct WeightsCall {
     const int32_t *cache_len, *vis;
     const float* lse;
     float* ws;
+    int rows, parts;                                   // rows of a part, parts of a cache
+    int chunk, splits;                                 // queries of a block, blocks that share them (more than 64 queries)
+    int pitch;                                         // of the logits that are kept
+    size_t off_ml, off_logits, off_lse, off_sums;      // floats
 };
-size_t weights_workspace(const WeightsCall& c, bool lse_given);   // floats
+size_t weights_workspace(WeightsCall& c, bool lse_given);   // floats; fills what follows ws
 nats_status launch_cache_weights(const WeightsCall& c, hipStream_t st);
 
 struct EvictCall {

@@ -32,7 +32,7 @@ static nats_status check_cache(int dtype, int B, int H, int d, int cap, long lon
     }
     if (d != 64 && d != 128) { set_error("d must be 64 or 128 (got %d)", d); return NATS_ERR_SHAPE; }
     if (heads > 65535) { set_error("the number of (batch, head) pairs must not exceed 65535 (got %lld)", heads); return NATS_ERR_SHAPE; }
-    if (cap > 1 << 23) { set_error("cap must not exceed 2^23 (got %d)", cap); return NATS_ERR_SHAPE; }
+    if (cap > 1 << 20) { set_error("cap must not exceed 2^20 (got %d)", cap); return NATS_ERR_SHAPE; }
     return NATS_OK;
 }
 
@@ -66,8 +66,8 @@ static nats_status check_weights_params(const nats_cache_weights_params* p) {
     if (p == nullptr) { set_error("params is NULL"); return NATS_ERR_NULL; }
     const nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, (long long)p->B * p->H);
     if (st != NATS_OK) return st;
-    if (p->T <= 0 || (long long)p->B * p->H * p->T > (1ll << 31) - 1) {
-        set_error("T must be positive and B*H*T fit in 31 bits (T %d)", p->T);
+    if (p->T <= 0 || p->T > 1 << 20 || (long long)p->B * p->H * p->T > (1ll << 31) - 1) {
+        set_error("T must be between 1 and 2^20 and B*H*T fit in 31 bits (T %d)", p->T);
         return NATS_ERR_SHAPE;
     }
     if (p->q_group < 0 || p->vis_group < 0 || (p->q_group && p->H % p->q_group) || (p->vis_group && p->H % p->vis_group)) {

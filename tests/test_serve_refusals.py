@@ -47,7 +47,7 @@ def commit(lib, p, a=None):
 
 
 BAD_TREES = [(dict(T=0), E_SHAPE), (dict(T=65), E_SHAPE), (dict(T=-1), E_SHAPE), (dict(B=0), E_SHAPE), (dict(H=-2), E_SHAPE),
-             (dict(d=96), E_SHAPE), (dict(cap=0), E_SHAPE), (dict(cap=(1 << 23) + 1), E_SHAPE), (dict(dtype=2), E_DTYPE),
+             (dict(d=96), E_SHAPE), (dict(cap=0), E_SHAPE), (dict(cap=(1 << 20) + 1), E_SHAPE), (dict(dtype=2), E_DTYPE),
              (dict(group=9), E_SHAPE), (dict(group=-1), E_SHAPE), (dict(B=40000, group=1), E_SHAPE), (dict(B=9000, group=8), E_SHAPE),
              (dict(combine_mode=3), E_SHAPE), (dict(linear_op=2), E_SHAPE), (dict(freeze_on_softmax=2), E_SHAPE)]
 
@@ -96,7 +96,7 @@ def weights(lib, p, a=None, ws=FAKE + 65536, size=1 << 40):
 
 @pytest.mark.parametrize("over,code", [(dict(T=0), E_SHAPE), (dict(d=80), E_SHAPE), (dict(cap=0), E_SHAPE), (dict(dtype=7), E_DTYPE),
                                        (dict(B=0), E_SHAPE), (dict(q_group=4), E_SHAPE), (dict(vis_group=5), E_SHAPE),
-                                       (dict(q_group=-1), E_SHAPE), (dict(T=1 << 30), E_SHAPE), (dict(B=20000), E_SHAPE)])
+                                       (dict(q_group=-1), E_SHAPE), (dict(B=1, H=1, T=(1 << 20) + 1), E_SHAPE), (dict(B=20000), E_SHAPE)])
 def test_weights_params(lib, over, code):
     assert weights(lib, weights_params(**over)) == code
     assert lib.nats_cache_weights_workspace_bytes(ctypes.byref(weights_params(**over)), 0) == 0
