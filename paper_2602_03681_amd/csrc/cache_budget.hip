@@ -1,6 +1,8 @@
 // Attention weights that a cache's rows get (nats_cache_weights), and the eviction by them (nats_cache_evict).
 #include <math.h>
 
+#include <type_traits>
+
 #include "nats_common.h"
 #include "nats_serve.h"
 #include "serve.h"
@@ -425,9 +427,7 @@ nats_status launch_cache_weights(const WeightsCall& c, hipStream_t st) {
     return c.d == 64 ? run_weights<bf16_t, 64>(c, st) : run_weights<bf16_t, 128>(c, st);
 }
 
-// ---- eviction: which rows stay ----
-constexpr int EV_THREADS = 1024;
-
+// ---- eviction: which rows stay ---------------------------------------------------------------------------------------------
 // A number that orders as the weights do (a NaN below all, -0 as 0)
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 0;
@@ -435,97 +435,171 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// exclusive prefix sum of an int over the block and its total
-__device__ __forceinline__ int block_scan(int x, int* s_part, int& total) {
-    const int tid = threadIdx.x, incl = wave_inclusive_scan_i32(x);
-    __syncthreads();   // s_part of the scan before has been read
-    if ((tid & 63) == 63) s_part[tid >> 6] = incl;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int w = 0; w < EV_THREADS / 64; ++w) {
-        if (w < (tid >> 6)) before += s_part[w];
-        total += s_part[w];
-    }
-    return before + incl - x;
-}
-
-// One block per cache.  The weight of the last row that stays is found digit by digit (8 bits of its key at a time, from counts of the
-// rows that agree in the digits so far); then the rows above it, the lowest of those equal to it and the last `recent` ones are
-// numbered in order, and their weights moved.  A row's new place is never behind its old one, and a step's rows are read before
-// any of them is written, so that the weights are compacted in place.
-__global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictCall c) {
-    __shared__ int s_hist[256], s_part[EV_THREADS / 64];
+// One block per cache.  The weight of the last row that stays is found digit by digit: 8 bits of its key at a time, from counts of the
+// rows that agree in the digits so far.  Then the rows above it, the lowest of those equal to it and the last `recent` ones are
+// numbered in order, and their weights moved.  The counts are kept in four copies, a lane's by its number: the first digit of attention weights
+// takes a dozen values, and lanes that add to one address go one after the other.  A wavefront has PER x 64 rows in a row, so that ranks inside it are counts of ballot bits.
+// Up to THREADS x PER rows the weights stay in registers throughout; longer caches are gone through in such steps, once per digit
+// and once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its old one).
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
+    constexpr int WAVES = THREADS / 64, STEP = THREADS * PER;
+    __shared__ int4 s_hist[256];   // copy lane % 4 of every count
+    __shared__ int s_ties[WAVES], s_stay[WAVES], s_rest;
     __shared__ uint32_t s_digit;
-    __shared__ int s_rest;
-    const int bh = blockIdx.x, tid = threadIdx.x;
+    const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = min(max(c.cache_len[bh], 0), c.cap);
     float* w = c.weights + (size_t)bh * c.cap;
     int32_t* kept = c.kept + (size_t)bh * c.keep;
     if (n <= c.keep) {
-        for (int r = tid; r < c.keep; r += EV_THREADS) kept[r] = r < n ? r : -1;
+        for (int r = tid; r < c.keep; r += THREADS) kept[r] = r < n ? r : -1;
         return;
     }
-    const int m = n - c.recent;   // the rows to choose from
+    const int m = n - c.recent;     // the rows to choose from
+    int rest = c.keep - c.recent;   // of those that agree with `prefix`, this many stay
+    const bool any = rest > 0, one = n <= STEP;
+    const int first = wave * 64 * PER + lane;
+    float x[PER];
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = r0 + first + 64 * i;
+            x[i] = r < n ? w[r] : 0.f;
+        }
+    };
+    if (one) load(0);
     uint32_t prefix = 0;
-    int rest = c.keep - c.recent;   // of the rows that agree with `prefix`, this many stay
-    if (rest > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += EV_THREADS) s_hist[i] = 0;
-            __syncthreads();
-            for (int r = tid; r < m; r += EV_THREADS) {
-                const uint32_t key = weight_key(w[r]);
-                if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(key >> shift) & 255], 1);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int d = 255, left = rest;
-                while (d > 0 && s_hist[d] < left) left -= s_hist[d--];
-                s_digit = d;
-                s_rest = left;
-            }
-            __syncthreads();
-            prefix |= s_digit << shift;
-            rest = s_rest;
-            __syncthreads();
-        }
-    }
-    int done = 0, equal = 0;   // rows that stay and rows equal to the threshold so far
-    const bool any = c.keep > c.recent;
-    for (int r0 = 0; r0 < n; r0 += EV_THREADS) {
-        const int r = r0 + tid;
-        const float x = r < n ? w[r] : 0.f;
-        const uint32_t key = weight_key(x);
-        const bool tie = r < m && any && key == prefix;
-        int ties, all;
-        const int rank = equal + block_scan(tie, s_part, ties);
-        const bool stays = r < n && (r >= m || (any && (key > prefix || (tie && rank < rest))));
-        const int at = done + block_scan(stays, s_part, all);   // (every thread has read its weight)
-        if (stays) {
-            w[at] = x;
-            kept[at] = r;
-        }
-        done += all;
-        equal += ties;
+    for (int shift = 24; any && shift >= 0; shift -= 8) {
+        for (int i = tid; i < 256; i += THREADS) s_hist[i] = make_int4(0, 0, 0, 0);
         __syncthreads();
+        for (int r0 = 0; r0 < m; r0 += STEP) {
+            if (!one) load(r0);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t key = weight_key(x[i]);
+                if (r0 + first + 64 * i < m && (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))))
+                    atomicAdd(reinterpret_cast<int*>(&s_hist[(key >> shift) & 255]) + (lane & 3), 1);
+            }
+        }
+        __syncthreads();
+        if (wave == 0) {   // lane l: digits 255 - 4 l and the three below it
+            int h[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int4 x = s_hist[255 - 4 * lane - i];
+                sum += h[i] = x.x + x.y + x.z + x.w;
+            }
+            int above = wave_inclusive_scan_i32(sum) - sum;
+            if (above < rest && rest <= above + sum) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (above < rest && rest <= above + h[i]) {
+                        s_digit = 255 - 4 * lane - i;
+                        s_rest = rest - above;
+                    }
+                    above += h[i];
+                }
+            }
+        }
+        __syncthreads();
+        prefix |= s_digit << shift;
+        rest = s_rest;
+    }
+    int done = 0, equal = 0;   // rows that stay, and rows equal to the last weight that stays, of the steps before
+    const uint64_t below = (1ull << lane) - 1;
+    for (int r0 = 0; r0 < n; r0 += STEP) {
+        if (!one) load(r0);
+        auto ties = [&](int i) { return any && r0 + first + 64 * i < m && weight_key(x[i]) == prefix; };
+        int n_ties = 0, n_stay = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) n_ties += __popcll(__ballot(ties(i)));
+        if (lane == 0) s_ties[wave] = n_ties;
+        __syncthreads();
+        int rank = equal;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) {
+            if (v < wave) rank += s_ties[v];
+            equal += s_ties[v];
+        }
+        uint32_t stays = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int r = r0 + first + 64 * i;
+            const bool tie = ties(i);
+            const uint64_t b = __ballot(tie);
+            const bool stay = r < n && (r >= m || (any && (weight_key(x[i]) > prefix || (tie && rank + __popcll(b & below) < rest))));
+            rank += __popcll(b);
+            stays |= stay ? 1u << i : 0u;
+            n_stay += __popcll(__ballot(stay));
+        }
+        if (lane == 0) s_stay[wave] = n_stay;
+        __syncthreads();   // (every weight of the step has been read)
+        int at = done;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) {
+            if (v < wave) at += s_stay[v];
+            done += s_stay[v];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const bool stay = (stays >> i) & 1;
+            const uint64_t b = __ballot(stay);
+            if (stay) {
+                const int to = at + __popcll(b & below);
+                w[to] = x[i];
+                kept[to] = r0 + first + 64 * i;
+            }
+            at += __popcll(b);
+        }
     }
     if (tid == 0) c.cache_len[bh] = c.keep;
 }
 
-// ---- eviction: the rows move ----
-// A block per cache, K or V, and slice of 64 bytes of the rows; rows in order, a step's rows read before any of them is written.
-constexpr int MV_THREADS = 256, MV_ROWS = MV_THREADS / 4;
-__global__ __launch_bounds__(MV_THREADS) void evict_move_kernel(EvictCall c, int row_bytes) {
-    const int bh = blockIdx.y, slice = blockIdx.x, slices = row_bytes / 64, tid = threadIdx.x;
-    char* base = (char*)(slice < slices ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + (slice % slices) * 64 + (tid & 3) * 16;
+// ---- eviction: the rows move ---------------------------------------------------------------------------------------------------
+// A block per cache, K or V, and slice of SLICE bytes of the rows, its rows in order.  Row r comes from kept[r] >= r, and kept rises: what a
+// step reads lies at or behind the rows it writes, so a step's rows are all read before any of them is written (the barrier), and the next
+// step's, which lie behind all that this one writes, are on their way meanwhile.
+constexpr int MV_WORDS = 8;   // 16-byte words per thread and step
+template <int SLICE, int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int row_bytes) {
+    constexpr int LANES = SLICE / 16, PER_WORD = THREADS / LANES, STEP = PER_WORD * MV_WORDS;   // rows
+    const int bh = blockIdx.x, slices = row_bytes / SLICE, tid = threadIdx.x;
+    const int array = blockIdx.y / slices, slice = blockIdx.y % slices;
+    char* base = (char*)(array == 0 ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + slice * SLICE + (tid % LANES) * 16;
     const int32_t* kept = c.kept + (size_t)bh * c.keep;
-    for (int r0 = 0; r0 < c.keep; r0 += MV_ROWS) {
-        const int r = r0 + (tid >> 2), src = r < c.keep ? kept[r] : -1;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (src > r) x = *reinterpret_cast<const uint4*>(base + (size_t)src * row_bytes);
-        asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));   // the row has arrived before the barrier
+    const int mine = tid / LANES;
+    uint4 now[MV_WORDS], next[MV_WORDS];
+    int src[MV_WORDS], src_next[MV_WORDS];
+    auto sources = [&](int r0, int (&s)[MV_WORDS]) {
+#pragma unroll
+        for (int i = 0; i < MV_WORDS; ++i) {
+            const int r = r0 + mine + i * PER_WORD;
+            s[i] = kept[min(r, c.keep - 1)];
+            s[i] = r < c.keep && s[i] > r ? s[i] : -1;   // (a row that stays where it is is not touched)
+        }
+    };
+    auto rows = [&](const int (&s)[MV_WORDS], uint4 (&x)[MV_WORDS]) {
+#pragma unroll
+        for (int i = 0; i < MV_WORDS; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (s[i] >= 0) x[i] = *reinterpret_cast<const uint4*>(base + (size_t)s[i] * row_bytes);
+        }
+    };
+    sources(0, src);
+    rows(src, now);
+    sources(STEP, src_next);
+    for (int r0 = 0; r0 < c.keep; r0 += STEP) {
+        rows(src_next, next);
+#pragma unroll
+        for (int i = 0; i < MV_WORDS; ++i) asm volatile("" : "+v"(now[i].x), "+v"(now[i].y), "+v"(now[i].z), "+v"(now[i].w));   // they are here
         __syncthreads();
-        if (src > r) *reinterpret_cast<uint4*>(base + (size_t)r * row_bytes) = x;
+#pragma unroll
+        for (int i = 0; i < MV_WORDS; ++i) {
+            if (src[i] >= 0) *reinterpret_cast<uint4*>(base + (size_t)(r0 + mine + i * PER_WORD) * row_bytes) = now[i];
+            now[i] = next[i];
+            src[i] = src_next[i];
+        }
+        sources(r0 + 2 * STEP, src_next);
     }
 }
 
@@ -533,10 +607,22 @@ nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
     const int heads = c.B * c.H, row_bytes = c.d * (c.dtype == NATS_F32 ? 4 : 2);
     {
         ProfScope ps("evict_select", st);
-        hipLaunchKernelGGL(evict_select_kernel, dim3(heads), dim3(EV_THREADS), 0, st, c);
+        if (c.cap <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(heads), dim3(256), 0, st, c);
+        else if (c.cap <= 4096) hipLaunchKernelGGL((evict_select_kernel<256, 16>), dim3(heads), dim3(256), 0, st, c);
+        else hipLaunchKernelGGL((evict_select_kernel<1024, 32>), dim3(heads), dim3(1024), 0, st, c);
     }
     ProfScope ps("evict_move", st);
-    hipLaunchKernelGGL(evict_move_kernel, dim3(2 * row_bytes / 64, heads), dim3(MV_THREADS), 0, st, c, row_bytes);
+    // slices as wide as leave two blocks per CU; where even narrow ones do not, blocks of 1024 threads
+    auto move = [&](auto slice, auto threads) {
+        constexpr int SLICE = decltype(slice)::value, THREADS = decltype(threads)::value;
+        hipLaunchKernelGGL((evict_move_kernel<SLICE, THREADS>), dim3(heads, 2 * (row_bytes / SLICE)), dim3(THREADS), 0, st, c, row_bytes);
+    };
+    using std::integral_constant;
+    const int bytes = heads * 2 * row_bytes;   // of a row of all caches, K and V
+    if (row_bytes >= 256 && bytes >= 512 * 256) move(integral_constant<int, 256>{}, integral_constant<int, 256>{});
+    else if (bytes >= 512 * 128) move(integral_constant<int, 128>{}, integral_constant<int, 256>{});
+    else if (bytes >= 512 * 64) move(integral_constant<int, 64>{}, integral_constant<int, 256>{});
+    else move(integral_constant<int, 64>{}, integral_constant<int, 1024>{});
     return check_launch("cache_evict");
 }
 
