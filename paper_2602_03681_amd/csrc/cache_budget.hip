@@ -262,74 +262,97 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall 
     }
 }
 
-// ---- many queries: 16 KT rows stay in every wavefront's registers, the block's wavefronts share its queries ----
+// ---- many queries: 16 KT rows stay in every wavefront's registers, the queries stream ----
+// WK of the block's wavefronts take rows side by side and the same queries, the others other queries: one wavefront's tile of queries is in the
+// CU's cache for the next.  Bounds of the block's queries (at most CW_CHUNK) go through LDS first; the tiles before the first one that
+// sees a row of the block's are left out.  Two tiles of queries are in registers: one is on its way while the other is multiplied.
+constexpr int CW_CHUNK = 1024;
 template <typename T, int D>
 constexpr int many_tiles() { return sizeof(T) == 2 || D == 64 ? 4 : 2; }
 
-template <typename T, int D>
+template <typename T, int D, int WK>
 __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall c) {
-    constexpr int KT = many_tiles<T, D>();
-    __shared__ float s_sum[CW_WAVES][16 * KT];
-    const int bh = blockIdx.x, r0 = blockIdx.y * 16 * KT, split = blockIdx.z, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = rows_of(c, bh);
-    if (r0 >= n) return;
-    const T* Q = queries<T>(c, bh);
-    const float* lse = (c.lse != nullptr ? c.lse : c.ws + c.off_lse) + (size_t)bh * c.T;
-    const float scale2 = c.scale * LOG2E;
-    const int end = min((split + 1) * c.chunk, c.T);
-    Rows16<T, D> k[KT], q;
-#pragma unroll
-    for (int i = 0; i < KT; ++i) k[i].load((const T*)c.k_cache + (size_t)bh * c.cap * D, r0 + 16 * i, n - 1, l16, lq);
+    constexpr int KT = many_tiles<T, D>(), WQ = CW_WAVES / WK, ROWS = 16 * KT * WK;
+    __shared__ float s_L[CW_CHUNK], s_sum[WQ][ROWS];
+    __shared__ int s_vis[CW_CHUNK], s_first;
+    const int bh = blockIdx.x, split = blockIdx.z, tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % WK, wq = wave / WK;
+    const int n = rows_of(c, bh), block0 = blockIdx.y * ROWS, r0 = block0 + wk * 16 * KT;
+    if (block0 >= n) return;
+    const int t0 = split * c.chunk, here = min(c.chunk, c.T - t0);
+    const T* Q = queries<T>(c, bh) + (size_t)t0 * D;
+    const float* lse = (c.lse != nullptr ? c.lse : c.ws + c.off_lse) + (size_t)bh * c.T + t0;
+    float* sums = c.ws + c.off_sums + ((size_t)split * c.B * c.H + bh) * c.cap;
+    if (tid == 0) s_first = here;
+    __syncthreads();
+    int first = here;
+    for (int t = tid; t < (here + 15) / 16 * 16; t += CW_THREADS) {
+        const int at = min(t, here - 1);
+        const float x = lse[at];
+        // queries that are not there, or whose lse is -inf, see nothing
+        const int vis = t < here && x != -INFINITY ? sees_rows(c, bh, t0 + at, n) : 0;
+        s_L[t] = x * LOG2E;
+        s_vis[t] = vis;
+        if (vis > block0) first = min(first, t);
+    }
+    first = wave_extreme_i32<false>(first);
+    if (lane == 0) atomicMin(&s_first, first);
+    __syncthreads();
+    first = s_first / 16 * 16;
     float sum[KT];
 #pragma unroll
     for (int i = 0; i < KT; ++i) sum[i] = 0.f;
-    int t = split * c.chunk + 16 * wave;
-    f32x4 L, nextL;
-    int vis[4], next_vis[4];
-    q.load(Q, t, c.T - 1, l16, lq);
-    query_bounds(c, lse, bh, t + 4 * lq, n, L, vis);
-    for (; t < end; t += 16 * CW_WAVES) {
-        const int least = min(min(vis[0], vis[1]), min(vis[2], vis[3])), most = max(max(vis[0], vis[1]), max(vis[2], vis[3]));
-        const bool any = __any(most > r0), all = __all(least >= r0 + 16 * KT);
-        f32x4 s[KT];
-        if (any) {
+    if (first < here && r0 < n) {
+        const float scale2 = c.scale * LOG2E;
+        Rows16<T, D> k[KT], q[2];
+        int t = first + 16 * wq;
 #pragma unroll
-            for (int i = 0; i < KT; ++i) s[i] = Rows16<T, D>::product(q, k[i]);
-        }
-        q.load(Q, t + 16 * CW_WAVES, c.T - 1, l16, lq);
-        query_bounds(c, lse, bh, t + 16 * CW_WAVES + 4 * lq, n, nextL, next_vis);
-        if (all) {
+        for (int i = 0; i < KT; ++i) k[i].load((const T*)c.k_cache + (size_t)bh * c.cap * D, r0 + 16 * i, n - 1, l16, lq);
+        q[0].load(Q, t, here - 1, l16, lq);
+        q[1].load(Q, t + 16 * WQ, here - 1, l16, lq);
+        while (t < here) {
 #pragma unroll
-            for (int i = 0; i < KT; ++i)
+            for (int u = 0; u < 2; ++u) {
+                const int at = min(t, (here - 1) / 16 * 16) + 4 * lq;   // (past the end: the last tile, which then counts for nothing)
+                const f32x4 L = *reinterpret_cast<const f32x4*>(&s_L[at]);
+                const int4 vis = *reinterpret_cast<const int4*>(&s_vis[at]);
+                const int least = min(min(vis.x, vis.y), min(vis.z, vis.w)), most = max(max(vis.x, vis.y), max(vis.z, vis.w));
+                const bool any = t < here && __any(most > r0), all = __all(least >= r0 + 16 * KT);
+                f32x4 s[KT];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[i] += __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
-        } else if (any) {
+                for (int i = 0; i < KT; ++i) s[i] = Rows16<T, D>::product(q[u], k[i]);
+                q[u].load(Q, t + 32 * WQ, here - 1, l16, lq);
+                if (any && all) {
 #pragma unroll
-            for (int i = 0; i < KT; ++i)
+                    for (int i = 0; i < KT; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
-                    sum[i] += r0 + 16 * i + l16 < vis[j] ? p : 0.f;
+                        for (int j = 0; j < 4; ++j) sum[i] += __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
+                } else if (any) {
+                    const int v[4] = {vis.x, vis.y, vis.z, vis.w};
+#pragma unroll
+                    for (int i = 0; i < KT; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float p = __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
+                            sum[i] += r0 + 16 * i + l16 < v[j] ? p : 0.f;
+                        }
                 }
+                t += 16 * WQ;
+            }
         }
-        L = nextL;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) vis[j] = next_vis[j];
     }
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
         sum[i] += lane_xor16(sum[i], lane);
         sum[i] += lane_xor32(sum[i], lane);
-        if (lq == 0) s_sum[wave][16 * i + l16] = sum[i];
+        if (lq == 0) s_sum[wq][wk * 16 * KT + 16 * i + l16] = sum[i];
     }
     __syncthreads();
-    const int r = r0 + (int)threadIdx.x;
-    if (threadIdx.x >= 16 * KT || r >= n) return;
-    float x = s_sum[0][threadIdx.x];
+    if (tid >= ROWS || block0 + tid >= n) return;
+    float x = s_sum[0][tid];
 #pragma unroll
-    for (int w = 1; w < CW_WAVES; ++w) x += s_sum[w][threadIdx.x];
-    c.ws[c.off_sums + ((size_t)split * c.B * c.H + bh) * c.cap + r] = x;
+    for (int w = 1; w < WQ; ++w) x += s_sum[w][tid];
+    sums[block0 + tid] = x;
 }
 
 // the splits' sums onto the weights, in order
@@ -363,10 +386,11 @@ size_t weights_workspace(WeightsCall& c, bool lse_given) {
         }
     }
     if (c.T > CW_FEW) {
-        // queries per block: as many as leave enough blocks
+        // rows of a block: those of up to four wavefronts, as the caches have them; queries: as many as leave enough blocks
         const int tiles = 16 * (c.dtype == NATS_BF16 || c.d == 64 ? 4 : 2);
-        const long long blocks = heads * ((c.cap + tiles - 1) / tiles);
-        c.chunk = 2048;
+        c.row_waves = c.cap <= tiles ? 1 : c.cap <= 2 * tiles ? 2 : 4;
+        const long long blocks = heads * ((c.cap + c.row_waves * tiles - 1) / (c.row_waves * tiles));
+        c.chunk = CW_CHUNK;
         while (c.chunk > 128 && blocks * ((c.T + c.chunk - 1) / c.chunk) < 2048) c.chunk /= 2;
         c.splits = (c.T + c.chunk - 1) / c.chunk;
         c.off_sums = at;
@@ -415,7 +439,10 @@ static nats_status run_weights(const WeightsCall& c, hipStream_t st) {
     {
         ProfScope ps("weights_many", st);
         constexpr int ROWS = 16 * many_tiles<T, D>();
-        hipLaunchKernelGGL((weights_many_kernel<T, D>), dim3(heads, (c.cap + ROWS - 1) / ROWS, c.splits), block, 0, st, c);
+        const dim3 grid(heads, (c.cap + c.row_waves * ROWS - 1) / (c.row_waves * ROWS), c.splits);
+        if (c.row_waves == 1) hipLaunchKernelGGL((weights_many_kernel<T, D, 1>), grid, block, 0, st, c);
+        else if (c.row_waves == 2) hipLaunchKernelGGL((weights_many_kernel<T, D, 2>), grid, block, 0, st, c);
+        else hipLaunchKernelGGL((weights_many_kernel<T, D, 4>), grid, block, 0, st, c);
     }
     ProfScope ps("weights_join", st);
     hipLaunchKernelGGL(weights_join_kernel, rows, block, 0, st, c);

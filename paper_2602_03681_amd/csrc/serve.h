@@ -53,7 +53,8 @@ struct WeightsCall {
     const float* lse;
     float* ws;
     int rows, parts;                                   // rows of a part, parts of a cache
-    int chunk, splits;                                 // queries of a block, blocks that share them (more than 64 queries)
+    int row_waves, chunk, splits;                      // more than 64 queries: wavefronts of a block that take rows side by side, its
+                                                       // queries, blocks that share a head's queries
     int pitch;                                         // of the logits that are kept
     size_t off_ml, off_logits, off_lse, off_sums;      // floats
 };
