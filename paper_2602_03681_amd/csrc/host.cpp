@@ -15,6 +15,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -22,6 +23,7 @@
 #include <initializer_list>
 
 #include "nats.h"
+#include "nats_serve.h"
 
 namespace {
 
@@ -230,9 +232,207 @@ PyObject* decode_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the calls of nats_serve.h: tensors on the current device only ----
+struct Here {
+    c10::DeviceIndex device = -1;   // asked for behind the first tensor that is on a GPU: without one there is no device to ask for
+    void* operator()(const at::Tensor& t, at::ScalarType dt, std::initializer_list<int64_t> shape) {
+        void* const p = pointer(t, dt, shape);
+        if (device < 0) device = c10::hip::current_device();
+        if (t.device().index() != device) throw NotTaken();
+        return p;
+    }
+    void* operator()(PyObject* o, at::ScalarType dt, std::initializer_list<int64_t> shape) { return (*this)(tensor(o), dt, shape); }
+    void* optional(PyObject* o, at::ScalarType dt, std::initializer_list<int64_t> shape) {
+        return o == Py_None ? nullptr : (*this)(o, dt, shape);
+    }
+    // the caller's workspace, or one made for the call
+    void* workspace(PyObject* given, at::Tensor& own, const at::Tensor& like, size_t need, size_t& bytes) {
+        if (given == Py_None) {
+            bytes = need;
+            if (need == 0) return nullptr;
+            own = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+            return own.data_ptr();
+        }
+        const at::Tensor& t = tensor(given);
+        if (!t.is_cuda() || t.layout() != at::kStrided || !t.is_contiguous() || t.device().index() != device) throw NotTaken();
+        bytes = (size_t)t.numel();
+        return t.data_ptr();
+    }
+};
+
+at::Tensor given_or_new(PyObject* o, std::initializer_list<int64_t> shape, const at::Tensor& like, at::ScalarType dt) {
+    return o == Py_None ? at::empty(at::IntArrayRef(shape.begin(), shape.size()), like.options().dtype(dt)) : tensor(o);
+}
+
+// B, H, T, d, cap, dtype, group of a call on a tree (k [B,H,T,d], k_cache [B,H group,cap,d])
+void tree_sizes(nats_tree_params& p, const at::Tensor& k, const at::Tensor& kc, int group) {
+    if (kc.dim() != 4 || k.dim() != 4 || group < 1 || k.size(1) * group != kc.size(1)) throw NotTaken();
+    p.B = (int)kc.size(0); p.H = (int)k.size(1); p.T = (int)k.size(2); p.d = (int)kc.size(3); p.cap = (int)kc.size(2);
+    p.dtype = dtype_code(kc.scalar_type());
+    p.group = group;
+}
+
+// decode_tree(state, k_cache, v_cache, cache_len, q, k, v, alpha, beta, mask, parent, n_nodes, q_nla, k_nla, w_nla, w_la, out, lse,
+//             workspace, softmax_scale, la_scale, combine_mode, rms_eps, linear_op, freeze_on_softmax, group) -> (out, lse)
+PyObject* decode_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 26) throw NotTaken();
+        Here here;
+        const at::Tensor &kc = tensor(a[1]), &k = tensor(a[5]), &v = tensor(a[6]);
+        nats_tree_params p{};
+        tree_sizes(p, k, kc, integer(a[25]));
+        const int64_t B = p.B, H = p.H, T = p.T, d = p.d, cap = p.cap, HG = kc.size(1);
+        const at::ScalarType dt = kc.scalar_type();
+        void* state = here(a[0], at::kFloat, {B, HG, d, d});
+        void* kcache = here(kc, dt, {B, HG, cap, d});
+        void* vcache = here(a[2], dt, {B, HG, cap, d});
+        void* len = here(a[3], at::kInt, {B, HG});
+        void* qp = here(a[4], dt, {B, H, T, d});
+        void* kp = here(k, dt, {B, H, T, d});
+        void* vp = here(v, dt, {B, HG, T, d});
+        void* alpha = here(a[7], at::kFloat, {B, H, T});
+        void* beta = here(a[8], at::kFloat, {B, H, T});
+        void* mask = here(a[9], at::kByte, {B, H, T});
+        void* parent = here(a[10], at::kInt, {B, T});
+        void* nodes = here.optional(a[11], at::kInt, {B});
+        p.q_nla = here.optional(a[12], dt, {B, HG, T, d});
+        p.k_nla = here.optional(a[13], dt, {B, HG, T, d});
+        void* wn = here.optional(a[14], at::kFloat, {B, HG, T});
+        void* wl = here.optional(a[15], at::kFloat, {B, HG, T});
+        p.softmax_scale = (float)number(a[19]);
+        p.la_scale = (float)number(a[20]);
+        p.combine_mode = integer(a[21]);
+        p.rms_eps = (float)number(a[22]);
+        p.linear_op = integer(a[23]);
+        p.freeze_on_softmax = integer(a[24]);
+        const at::Tensor out = given_or_new(a[16], {B, HG, T, d}, v, dt), lse = given_or_new(a[17], {B, HG, T}, v, at::kFloat);
+        void* op = here(out, dt, {B, HG, T, d});
+        void* lp = here(lse, at::kFloat, {B, HG, T});
+        at::Tensor own;
+        size_t bytes = 0;
+        const size_t need = a[18] == Py_None ? nats_hybrid_attn_decode_tree_workspace_bytes(&p) : 0;
+        void* const ws = here.workspace(a[18], own, v, need, bytes);
+        void* const stream = current_stream();
+        const nats_status st = unlocked([&] {
+            return nats_hybrid_attn_decode_tree(&p, (const float*)state, kcache, vcache, (const int32_t*)len, qp, kp, vp, (const float*)alpha,
+                                                (const float*)beta, (const uint8_t*)mask, (const int32_t*)parent, (const int32_t*)nodes,
+                                                (const float*)wn, (const float*)wl, op, (float*)lp, ws, bytes, stream);
+        });
+        if (st != NATS_OK) return PyLong_FromLong(st);
+        PyObject* pair[2] = {THPVariable_Wrap(out), THPVariable_Wrap(lse)};
+        PyObject* const r = pair[0] && pair[1] ? PyTuple_Pack(2, pair[0], pair[1]) : nullptr;
+        Py_XDECREF(pair[0]);
+        Py_XDECREF(pair[1]);
+        return r;
+    });
+}
+
+// tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, k_nla, vis, err_flags, linear_op,
+//             freeze_on_softmax, group) -> vis
+PyObject* tree_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 17) throw NotTaken();
+        Here here;
+        const at::Tensor &kc = tensor(a[1]), &k = tensor(a[4]), &v = tensor(a[5]);
+        nats_tree_params p{};
+        tree_sizes(p, k, kc, integer(a[16]));
+        const int64_t B = p.B, H = p.H, T = p.T, d = p.d, cap = p.cap, HG = kc.size(1);
+        const at::ScalarType dt = kc.scalar_type();
+        void* state = here(a[0], at::kFloat, {B, HG, d, d});
+        void* kcache = here(kc, dt, {B, HG, cap, d});
+        void* vcache = here(a[2], dt, {B, HG, cap, d});
+        void* len = here(a[3], at::kInt, {B, HG});
+        void* kp = here(k, dt, {B, H, T, d});
+        void* vp = here(v, dt, {B, HG, T, d});
+        void* alpha = here(a[6], at::kFloat, {B, H, T});
+        void* beta = here(a[7], at::kFloat, {B, H, T});
+        void* mask = here(a[8], at::kByte, {B, H, T});
+        void* parent = here(a[9], at::kInt, {B, T});
+        void* node = here(a[10], at::kInt, {B});
+        p.k_nla = here.optional(a[11], dt, {B, HG, T, d});
+        void* err = here.optional(a[13], at::kInt, {B, HG});
+        p.linear_op = integer(a[14]);
+        p.freeze_on_softmax = integer(a[15]);
+        const at::Tensor vis = given_or_new(a[12], {B, HG, T}, v, at::kInt);
+        void* visp = here(vis, at::kInt, {B, HG, T});
+        void* const stream = current_stream();
+        return status(unlocked([&] {
+            return nats_hybrid_attn_tree_commit(&p, (float*)state, kcache, vcache, (int32_t*)len, kp, vp, (const float*)alpha,
+                                                (const float*)beta, (const uint8_t*)mask, (const int32_t*)parent, (const int32_t*)node,
+                                                (int32_t*)visp, (int32_t*)err, stream);
+        }), vis);
+    });
+}
+
+// cache_weights(weights, q, k_cache, cache_len, lse, vis, workspace, softmax_scale, decay) -> weights
+PyObject* cache_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 9) throw NotTaken();
+        Here here;
+        const at::Tensor &weights = tensor(a[0]), &q = tensor(a[1]), &kc = tensor(a[2]);
+        if (kc.dim() != 4 || q.dim() != 4) throw NotTaken();
+        const int64_t B = kc.size(0), H = kc.size(1), cap = kc.size(2), d = kc.size(3), Hq = q.size(1), T = q.size(2);
+        int64_t Hv = H;
+        if (a[5] != Py_None) {
+            if (tensor(a[5]).dim() != 3) throw NotTaken();
+            Hv = tensor(a[5]).size(1);
+        }
+        if (Hq == 0 || Hv == 0 || H % Hq || H % Hv) throw NotTaken();
+        const at::ScalarType dt = kc.scalar_type();
+        nats_cache_weights_params p{};
+        p.B = (int)B; p.H = (int)H; p.T = (int)T; p.d = (int)d; p.cap = (int)cap; p.dtype = dtype_code(dt);
+        p.q_group = (int)(H / Hq);
+        p.vis_group = (int)(H / Hv);
+        p.softmax_scale = (float)number(a[7]);
+        p.decay = (float)number(a[8]);
+        void* wp = here(weights, at::kFloat, {B, H, cap});
+        void* qp = here(q, dt, {B, Hq, T, d});
+        void* kp = here(kc, dt, {B, H, cap, d});
+        void* len = here(a[3], at::kInt, {B, H});
+        void* lse = here.optional(a[4], at::kFloat, {B, H, T});
+        void* vis = here.optional(a[5], at::kInt, {B, Hv, T});
+        at::Tensor own;
+        size_t bytes = 0;
+        const size_t need = a[6] == Py_None ? nats_cache_weights_workspace_bytes(&p, lse != nullptr) : 0;
+        void* const ws = here.workspace(a[6], own, q, need, bytes);
+        void* const stream = current_stream();
+        return status(unlocked([&] {
+            return nats_cache_weights(&p, (float*)wp, qp, kp, (const int32_t*)len, (const int32_t*)vis, (const float*)lse, ws, bytes, stream);
+        }), weights);
+    });
+}
+
+// cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent) -> kept
+PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 7) throw NotTaken();
+        Here here;
+        const at::Tensor& kc = tensor(a[0]);
+        if (kc.dim() != 4) throw NotTaken();
+        const int64_t B = kc.size(0), H = kc.size(1), cap = kc.size(2), d = kc.size(3);
+        const at::ScalarType dt = kc.scalar_type();
+        nats_cache_evict_params p{(int)B, (int)H, (int)d, (int)cap, dtype_code(dt), integer(a[5]), integer(a[6])};
+        if (p.keep < 1) throw NotTaken();
+        void* kp = here(kc, dt, {B, H, cap, d});
+        void* vp = here(a[1], dt, {B, H, cap, d});
+        void* len = here(a[2], at::kInt, {B, H});
+        void* wp = here(a[3], at::kFloat, {B, H, cap});
+        const at::Tensor kept = given_or_new(a[4], {B, H, (int64_t)p.keep}, kc, at::kInt);
+        void* keptp = here(kept, at::kInt, {B, H, (int64_t)p.keep});
+        void* const stream = current_stream();
+        return status(unlocked([&] {
+            return nats_cache_evict(&p, kp, vp, (int32_t*)len, (float*)wp, (int32_t*)keptp, stream);
+        }), kept);
+    });
+}
+
 PyMethodDef methods[] = {
     {"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, "nats_hybrid_attn_decode"},
     {"decode_chunk", (PyCFunction)(void (*)(void))decode_chunk, METH_FASTCALL, "nats_hybrid_attn_decode_chunk"},
+    {"decode_tree", (PyCFunction)(void (*)(void))decode_tree, METH_FASTCALL, "nats_hybrid_attn_decode_tree"},
+    {"tree_commit", (PyCFunction)(void (*)(void))tree_commit, METH_FASTCALL, "nats_hybrid_attn_tree_commit"},
+    {"cache_weights", (PyCFunction)(void (*)(void))cache_weights, METH_FASTCALL, "nats_cache_weights"},
+    {"cache_evict", (PyCFunction)(void (*)(void))cache_evict, METH_FASTCALL, "nats_cache_evict"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nats_host", "host path of the per-token calls", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

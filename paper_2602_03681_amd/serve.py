@@ -90,6 +90,14 @@ def hybrid_attn_decode_tree(state, k_cache, v_cache, cache_len, q, k, v, alpha, 
     [B,H,T,d], alpha, beta, mask [B,H,T]; everything else has H * group heads.  n_nodes [B] i32: nodes from there on give rows
     of 0 and lse -inf.  workspace: uint8 tensor of decode_tree_workspace_bytes(...) bytes, allocated for the call if None."""
     lib = nb.load_library()
+    r = nb._host.decode_tree(state, k_cache, v_cache, cache_len, q, k, v, alpha, beta, mask, parent, n_nodes, q_nla, k_nla, w_nla,
+                             w_la, out, lse, workspace, softmax_scale, la_scale, combine_mode, rms_eps, linear_op, freeze_on_softmax,
+                             group)
+    if r is not None:
+        if type(r) is int:
+            _check(r)
+        return r
+    # an argument that the host path does not take: the checks below say which
     B, H, T, d, cap, HG = _tree_shape(k, k_cache, group)
     dt = k_cache.dtype
     _require(state, "state", (B, HG, d, d), torch.float32)
@@ -134,6 +142,12 @@ def hybrid_attn_tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, bet
     """nats_hybrid_attn_tree_commit: the path to node [B] i32 (-1: nothing) is written into state, caches and cache_len, in place
     -> vis [B,H*G,T] i32, the rows of the cache that each node of the path saw (0: not on the path)."""
     lib = nb.load_library()
+    r = nb._host.tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, k_nla, vis, err_flags,
+                             linear_op, freeze_on_softmax, group)
+    if r is not None:
+        if type(r) is int:
+            _check(r)
+        return r
     B, H, T, d, cap, HG = _tree_shape(k, k_cache, group)
     dt = k_cache.dtype
     _require(state, "state", (B, HG, d, d), torch.float32)
@@ -166,6 +180,11 @@ def cache_weights(weights, q, k_cache, cache_len, *, lse=None, vis=None, softmax
     rows of the cache, in place.  Hq divides H (a query head serves H / Hq heads of the cache in a row), so does the number of heads
     of vis [B,Hv,T] i32 (rows that a query sees; None: all).  lse [B,H,T] f32: None: taken over the rows that a query sees."""
     lib = nb.load_library()
+    r = nb._host.cache_weights(weights, q, k_cache, cache_len, lse, vis, workspace, softmax_scale, decay)
+    if r is not None:
+        if type(r) is int:
+            _check(r)
+        return r
     B, H, cap, d = _cache_shape(k_cache)
     dt = k_cache.dtype
     if q.dim() != 4 or q.shape[1] == 0 or H % q.shape[1]:
@@ -195,6 +214,11 @@ def cache_evict(k_cache, v_cache, cache_len, weights, keep: int, recent: int = 0
     """nats_cache_evict: caches of more than `keep` rows keep their last `recent` rows and the heaviest of the others, in order and in
     place (k_cache, v_cache, weights, cache_len) -> kept [B,H,keep] i32, the row that each row was before (-1: no row)."""
     lib = nb.load_library()
+    r = nb._host.cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent)
+    if r is not None:
+        if type(r) is int:
+            _check(r)
+        return r
     B, H, cap, d = _cache_shape(k_cache)
     dt = k_cache.dtype
     _require(k_cache, "k_cache", (B, H, cap, d), dt)
