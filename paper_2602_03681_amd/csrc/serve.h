@@ -22,13 +22,15 @@ struct TreeCall {
     void* o;
     float* lse;
     float* ws;
-    int rows, n_split;                         // rows of a part, parts of a cache
-    size_t off_ola, off_part, off_ml;   // floats
+    int rows, n_split;                          // rows of a part, parts of a cache
+    size_t off_anc, off_ola, off_part, off_ml;  // floats
+    // [B][T] ancestor sets, from the linear branch's blocks to the merge
+    __host__ __device__ uint64_t* anc() const { return reinterpret_cast<uint64_t*>(ws + off_anc); }
 };
 size_t tree_workspace(TreeCall& c);    // floats; fills rows, n_split and the offsets
 nats_status launch_tree(const TreeCall& c, hipStream_t st);
 int tree_cache_rows(const TreeCall& c);
-nats_status launch_tree_cache(const TreeCall& c, hipStream_t st);
+nats_status launch_tree_read(const TreeCall& c, hipStream_t st);   // both branches
 
 struct TreeCommitCall {
     int B, H, G, T, d, cap, dtype;

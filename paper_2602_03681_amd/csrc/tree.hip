@@ -5,16 +5,9 @@
 #include "nats_common.h"
 #include "nats_serve.h"
 #include "serve.h"
-#include "tree_linear.h"
 #include "tree_nodes.h"
 
 namespace nats {
-
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(TL_THREADS) void tree_linear_kernel(TreeCall c) {
-    __shared__ LinearLds<NT> s;
-    tree_linear_block<T, D, NT>(c, blockIdx.x, s);
-}
 
 // ---- the parts, the node's softmax ancestors and the linear branch's row into the output: a wavefront per node and head ----
 constexpr int MERGE_THREADS = 256;
@@ -42,7 +35,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
     }
     const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
     const uint64_t soft = __ballot(lane < N && c.mask[(size_t)bh * N + min(lane, N - 1)] != 0);
-    const uint64_t sees = soft & shfl_u64(ancestors(parent_of(c.parent, b, N, lane), lane), t);
+    const uint64_t sees = soft & c.anc()[(size_t)b * N + t];
     // the nodes' logits, lane j for node j, in the parts' units (powers of 2)
     constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : (const T*)c.k + (size_t)bh * N * D;
@@ -199,8 +192,9 @@ size_t tree_workspace(TreeCall& c) {
     const size_t heads = (size_t)c.B * c.H * c.G;
     c.rows = tree_cache_rows(c);
     c.n_split = (c.cap + c.rows - 1) / c.rows;
-    c.off_ola = 0;
-    c.off_part = heads * c.T * c.d;
+    c.off_anc = 0;
+    c.off_ola = align_up((size_t)c.B * c.T * 2, 4);
+    c.off_part = c.off_ola + heads * c.T * c.d;
     c.off_ml = c.off_part + heads * c.n_split * c.T * c.d;
     return c.off_ml + heads * c.n_split * c.T * 2;
 }
@@ -208,13 +202,7 @@ size_t tree_workspace(TreeCall& c) {
 template <typename T, int D>
 static nats_status run_tree(const TreeCall& c, hipStream_t st) {
     const int heads = c.B * c.H * c.G;
-    {
-        ProfScope ps("tree_linear", st);
-        if (c.T <= 16) hipLaunchKernelGGL((tree_linear_kernel<T, D, 1>), dim3(heads), dim3(TL_THREADS), 0, st, c);
-        else if (c.T <= 32) hipLaunchKernelGGL((tree_linear_kernel<T, D, 2>), dim3(heads), dim3(TL_THREADS), 0, st, c);
-        else hipLaunchKernelGGL((tree_linear_kernel<T, D, 4>), dim3(heads), dim3(TL_THREADS), 0, st, c);
-    }
-    const nats_status r = launch_tree_cache(c, st);
+    const nats_status r = launch_tree_read(c, st);
     if (r != NATS_OK) return r;
     constexpr int NODES = MERGE_THREADS / 64;
     ProfScope ps("tree_merge", st);

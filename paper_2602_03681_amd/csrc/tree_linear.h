@@ -39,8 +39,9 @@ struct LinearLds {
 
 __device__ __forceinline__ float4 as_float4(f32x4 x) { return make_float4(x[0], x[1], x[2], x[3]); }
 
-template <typename T, int D, int NT>
-__device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, LinearLds<NT>& s) {
+// TURNS x 64 rows of S, number `part` of them
+template <typename T, int D, int NT, int TURNS>
+__device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, int part, LinearLds<NT>& s) {
     constexpr int KS = D / 32;
     const int bh = bhg / c.G, b = bh / c.H, N = c.T, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -55,33 +56,40 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, Li
 #pragma unroll
         for (int i = 0; i < KS; ++i) sr[i].load(S + (size_t)(row0 + l16) * D + 32 * i + 8 * lq);
     };
-    load_state(16 * wave);
+    const int row0 = 16 * (part * TURNS * TL_WAVES + wave);   // of the wavefront's first turn
+    load_state(row0);
 
-    // ---- paths, their decays ----
-    if (wave == 0) {
-        const int there = c.n_nodes != nullptr ? min(c.n_nodes[b], N) : N, par = parent_of(c.parent, b, N, lane);
-        const bool soft = c.mask[(size_t)bh * N + min(lane, N - 1)] != 0;
-        float a = c.alpha[(size_t)bh * N + min(lane, N - 1)], bt = c.beta[(size_t)bh * N + min(lane, N - 1)];
-        if (lane >= N || (soft && c.freeze)) a = 1.f;
-        if (lane >= there || soft) bt = 0.f;
-        float g = a;
-        double lg = log2((double)a);
-        along_paths(par, lane, [&](bool up, int from) {
-            const float more = __shfl(g, from);
-            const uint64_t l = shfl_u64(__double_as_longlong(lg), from);
-            if (up) {
-                g *= more;
-                lg += __longlong_as_double(l);
-            }
-        });
-        const bool plain = __all(a > 0x1p-120f && a < 0x1p120f);
-        s.anc[lane] = ancestors(par, lane);
-        s.par[lane] = par;
-        s.a[lane] = a;
-        s.b[lane] = bt;
-        s.g[lane] = g;
-        s.lg[lane] = lg;
-        if (lane == 0) s.plain = plain;
+    // ---- paths (one wavefront), their decays (another) ----
+    if (wave < 2) {
+        const int par = parent_of(c.parent, b, N, lane);
+        if (wave == 0) {
+            const uint64_t anc = ancestors(par, lane);
+            s.anc[lane] = anc;
+            s.par[lane] = par;
+            if (lane < N && part == 0 && bhg % (c.H * c.G) == 0) c.anc()[(size_t)b * N + lane] = anc;   // for the merge
+        } else {
+            const int there = c.n_nodes != nullptr ? min(c.n_nodes[b], N) : N;
+            const bool soft = c.mask[(size_t)bh * N + min(lane, N - 1)] != 0;
+            float a = c.alpha[(size_t)bh * N + min(lane, N - 1)], bt = c.beta[(size_t)bh * N + min(lane, N - 1)];
+            if (lane >= N || (soft && c.freeze)) a = 1.f;
+            if (lane >= there || soft) bt = 0.f;
+            float g = a;
+            double lg = log2((double)a);
+            along_paths(par, lane, [&](bool up, int from) {
+                const float more = __shfl(g, from);
+                const uint64_t l = shfl_u64(__double_as_longlong(lg), from);
+                if (up) {
+                    g *= more;
+                    lg += __longlong_as_double(l);
+                }
+            });
+            const bool plain = __all(a > 0x1p-120f && a < 0x1p120f);
+            s.a[lane] = a;
+            s.b[lane] = bt;
+            s.g[lane] = g;
+            s.lg[lane] = lg;
+            if (lane == 0) s.plain = plain;
+        }
     }
 
     // ---- N and P: the lower triangle's tiles, dealt out to the wavefronts ----
@@ -155,8 +163,8 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, Li
     // ---- 16 columns at a time ----
     float* O = c.ws + c.off_ola + (size_t)bhg * N * D;
 #pragma unroll
-    for (int turn = 0; turn < D / (16 * TL_WAVES); ++turn) {
-        const int col = 16 * (turn * TL_WAVES + wave) + l16;
+    for (int turn = 0; turn < TURNS; ++turn) {
+        const int col = row0 + 16 * TL_WAVES * turn + l16;
         f32x4 w[NT], o[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -177,7 +185,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, Li
                 o[t] = mfma_terms(tx, ts, o[t]);
             }
         }
-        if (turn + 1 < D / (16 * TL_WAVES)) load_state(16 * ((turn + 1) * TL_WAVES + wave));
+        if (turn + 1 < TURNS) load_state(row0 + 16 * TL_WAVES * (turn + 1));
         f32x4 u[NT];
         bool fine = true;
 #pragma unroll

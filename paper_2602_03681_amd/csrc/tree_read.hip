@@ -1,5 +1,6 @@
-// Softmax branch of a tree of drafted tokens over the cache: partial results (running maximum m, sum l, weighted sum of V rows) of up to
-// 64 queries over a part of a cache's rows.
+// Both branches of a tree of drafted tokens, read in one launch: the first blocks take the linear branch (tree_linear.h), the others the
+// softmax branch over the cache: partial results (running maximum m, sum l, weighted sum of V rows) of up to 64 queries over a part of a
+// cache's rows.  Side by side the linear branch's dependent steps cost nothing where there are rows to read.
 //
 // Memory-bound: a cache row of 4 d (bf16) or 8 d bytes (fp32) feeds 4 d T operations, at most T = 64 per byte, against the 240 (bf16)
 // that a large product has per byte of a large copy on this card.  So all that matters is that every row is read once and that enough
@@ -21,6 +22,7 @@
 #include "nats_common.h"
 #include "serve.h"
 #include "softmax_terms.h"
+#include "tree_linear.h"
 
 namespace nats {
 
@@ -178,14 +180,20 @@ struct CacheTile<float, D> {
 constexpr int TC_THREADS = 256, TC_WAVES = TC_THREADS / 64;
 
 // NQ: tiles of 16 queries per wavefront; QG: groups of 16 NQ queries in a block, the block's other wavefronts share the rows
+template <int D, int NQ>
+struct CacheLds {
+    f32x4 o[2][NQ * (D / 16)][64];
+    float ml[2][NQ][2][64];
+};
+
 template <typename T, int D, int NQ, int QG>
-__global__ __launch_bounds__(TC_THREADS, 2) void tree_cache_kernel(TreeCall c) {
+__device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int split, CacheLds<D, NQ>& lds) {
     using Tile = CacheTile<T, D>;
     constexpr int KT = Tile::KT, ROWS = 16 * KT, KG = TC_WAVES / QG, E = D / 16;
     constexpr float LOG2E = 1.44269504088896341f;
-    __shared__ f32x4 s_o[2][NQ * E][64];
-    __shared__ float s_ml[2][NQ][2][64];
-    const int split = blockIdx.x, bhg = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    auto& s_o = lds.o;
+    auto& s_ml = lds.ml;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave / KG, kg = wave % KG;
     const int n = min(max(c.cache_len[bhg], 0), c.cap), lo = split * c.rows, last = min(n - lo, c.rows) - 1;
     if (last < 0) return;   // uniform: the merge knows from the same length which parts exist
@@ -304,12 +312,31 @@ __global__ __launch_bounds__(TC_THREADS, 2) void tree_cache_kernel(TreeCall c) {
     }
 }
 
-template <typename T, int D>
-static void run_tree_cache(const TreeCall& c, hipStream_t st) {
-    const dim3 grid(c.n_split, c.B * c.H * c.G), block(TC_THREADS);
-    if (c.T <= 16) hipLaunchKernelGGL((tree_cache_kernel<T, D, 1, 1>), grid, block, 0, st, c);
-    else if (c.T <= 32) hipLaunchKernelGGL((tree_cache_kernel<T, D, 2, 1>), grid, block, 0, st, c);
-    else hipLaunchKernelGGL((tree_cache_kernel<T, D, 2, 2>), grid, block, 0, st, c);
+static_assert(TC_THREADS == TL_THREADS, "blocks of either kind in one launch");
+
+template <typename T, int D, int NQ, int QG, int TURNS>
+__global__ __launch_bounds__(TC_THREADS, 2) void tree_read_kernel(TreeCall c) {
+    constexpr int PARTS = D / (64 * TURNS);   // blocks of a head's linear branch
+    __shared__ union {
+        LinearLds<NQ * QG> linear;
+        CacheLds<D, NQ> cache;
+    } s;
+    const int heads = c.B * c.H * c.G, id = blockIdx.x;
+    if (id < heads * PARTS) {
+        tree_linear_block<T, D, NQ * QG, TURNS>(c, id / PARTS, id % PARTS, s.linear);
+    } else {
+        const int x = id - heads * PARTS;
+        tree_cache_block<T, D, NQ, QG>(c, x / c.n_split, x % c.n_split, s.cache);
+    }
+}
+
+template <typename T, int D, int TURNS>
+static void run_tree_read(const TreeCall& c, hipStream_t st) {
+    const int heads = c.B * c.H * c.G;
+    const dim3 grid(heads * (D / (64 * TURNS)) + heads * c.n_split), block(TC_THREADS);
+    if (c.T <= 16) hipLaunchKernelGGL((tree_read_kernel<T, D, 1, 1, TURNS>), grid, block, 0, st, c);
+    else if (c.T <= 32) hipLaunchKernelGGL((tree_read_kernel<T, D, 2, 1, TURNS>), grid, block, 0, st, c);
+    else hipLaunchKernelGGL((tree_read_kernel<T, D, 2, 2, TURNS>), grid, block, 0, st, c);
 }
 
 // Rows of a part: as many as keep the partial results (4 T d bytes each, written and read) small beside the rows (4 d or 8 d bytes
@@ -321,11 +348,14 @@ int tree_cache_rows(const TreeCall& c) {
     return rows;
 }
 
-nats_status launch_tree_cache(const TreeCall& c, hipStream_t st) {
-    ProfScope ps("tree_cache", st);
-    if (c.dtype == NATS_F32) c.d == 64 ? run_tree_cache<float, 64>(c, st) : run_tree_cache<float, 128>(c, st);
-    else c.d == 64 ? run_tree_cache<bf16_t, 64>(c, st) : run_tree_cache<bf16_t, 128>(c, st);
-    return check_launch("tree_cache");
+nats_status launch_tree_read(const TreeCall& c, hipStream_t st) {
+    ProfScope ps("tree_read", st);
+    // d = 128 with few heads: a head's linear branch in two blocks, which is the shorter chain
+    const bool halves = (long long)c.B * c.H * c.G <= 128;
+    if (c.d == 64) c.dtype == NATS_F32 ? run_tree_read<float, 64, 1>(c, st) : run_tree_read<bf16_t, 64, 1>(c, st);
+    else if (halves) c.dtype == NATS_F32 ? run_tree_read<float, 128, 1>(c, st) : run_tree_read<bf16_t, 128, 1>(c, st);
+    else c.dtype == NATS_F32 ? run_tree_read<float, 128, 2>(c, st) : run_tree_read<bf16_t, 128, 2>(c, st);
+    return check_launch("tree_read");
 }
 
 }  // namespace nats
