@@ -2,6 +2,7 @@
 // path (nats_hybrid_attn_tree_commit).
 #include <math.h>
 
+#include "mfma_util.h"
 #include "nats_common.h"
 #include "nats_serve.h"
 #include "serve.h"
@@ -33,67 +34,102 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
         if (lane == 0 && c.lse != nullptr) c.lse[at] = -INFINITY;
         return;
     }
-    const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
-    const uint64_t soft = __ballot(lane < N && c.mask[(size_t)bh * N + min(lane, N - 1)] != 0);
-    const uint64_t sees = soft & c.anc()[(size_t)b * N + t];
-    // the nodes' logits, lane j for node j, in the parts' units (powers of 2)
+    // What does not depend on the number of parts is asked for at once, the first parts before it is known which there are (a part's place
+    // exists whatever the length; what it holds enters only if the part does).
+    constexpr int AHEAD = 4;
     constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : (const T*)c.k + (size_t)bh * N * D;
     const T* v = (const T*)c.v + (size_t)bhg * N * D;
-    float q[CPL], x = -INFINITY;
+    const size_t part0 = (size_t)bhg * c.n_split * N + t;
+    const float* rows = c.ws + c.off_part + part0 * D + lane * CPL;
+    const uint64_t anc = c.anc()[(size_t)b * N + t];
+    const bool is_soft = c.mask[(size_t)bh * N + min(lane, N - 1)] != 0;
+    float q[CPL], ahead[AHEAD][CPL], o_nla[CPL], o_la[CPL];
     columns(c.q_nla != nullptr ? (const T*)c.q_nla + at * D : (const T*)c.q + ((size_t)bh * N + t) * D, q);
-    for (uint64_t left = sees; left; left &= left - 1) {
-        const int j = __builtin_ctzll(left);
-        float k[CPL], dot = 0.f;
-        columns(ks + (size_t)j * D, k);
+    float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part0 + (size_t)min(lane, c.n_split - 1) * N) * 2);
 #pragma unroll
-        for (int i = 0; i < CPL; ++i) dot += q[i] * k[i];
-        dot = lane_group_sum<64>(dot);
-        if (lane == j) x = dot * (c.scale * LOG2E);
+    for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) ahead[s][i] = rows[(size_t)min(s, c.n_split - 1) * N * D + i];
+#pragma unroll
+    for (int i = 0; i < CPL; ++i) o_la[i] = c.ws[c.off_ola + at * D + lane * CPL + i];
+    const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
+    const uint64_t sees = anc & __ballot(lane < N && is_soft);
+
+    // the node's softmax ancestors, four at a time; logits in the parts' units (powers of 2), the same in every lane
+    float m = -INFINITY, l = 0.f, acc[CPL] = {};
+    for (uint64_t left = sees; left;) {
+        float k[4][CPL], x[4][CPL], z[4], top = m;
+        bool there[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            there[e] = left != 0;
+            const int j = there[e] ? __builtin_ctzll(left) : 0;
+            if (there[e]) left &= left - 1;
+            columns(ks + (size_t)j * D, k[e]);
+            columns(v + (size_t)j * D, x[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) dot += q[i] * k[e][i];
+            z[e] = there[e] ? lane_group_sum<64>(dot) * (c.scale * LOG2E) : -INFINITY;
+            top = fmaxf(top, z[e]);
+        }
+        const float ref = top == -INFINITY ? 0.f : top, was = __builtin_amdgcn_exp2f(m - ref);
+        m = top;
+        l *= was;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) acc[i] *= was;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (there[e]) {   // (uniform; a node that is not seen may hold anything)
+                const float p = __builtin_amdgcn_exp2f(z[e] - ref);
+                l += p;
+#pragma unroll
+                for (int i = 0; i < CPL; ++i) acc[i] += p * x[e][i];
+            }
     }
     auto top_of = [](float y) {
 #pragma unroll
         for (int w = 1; w < 64; w *= 2) y = fmaxf(y, __shfl_xor(y, w));
         return y;
     };
-    const bool mine = (sees >> lane) & 1;
-    float m = top_of(x), ref = m == -INFINITY ? 0.f : m;
-    float p = mine ? __builtin_amdgcn_exp2f(x - ref) : 0.f, l = lane_group_sum<64>(p), acc[CPL] = {};
-    for (uint64_t left = sees; left; left &= left - 1) {
-        const int j = __builtin_ctzll(left);
-        float vj[CPL];
-        columns(v + (size_t)j * D, vj);
-        const float pj = __shfl(p, j);
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) acc[i] += pj * vj[i];
-    }
     for (int first = 0; first < parts; first += 64) {
-        const size_t part = ((size_t)bhg * c.n_split + first) * N + t;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (first + lane < parts) ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part + (size_t)lane * N) * 2);
-        const float top = fmaxf(m, top_of(ml.x));
-        ref = top == -INFINITY ? 0.f : top;
+        if (first > 0 && first + lane < parts)
+            ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part0 + (size_t)(first + lane) * N) * 2);
+        if (first + lane >= parts) ml = make_float2(-INFINITY, 0.f);
+        const float top = fmaxf(m, top_of(ml.x)), ref = top == -INFINITY ? 0.f : top;
         const float was = __builtin_amdgcn_exp2f(m - ref), w = __builtin_amdgcn_exp2f(ml.x - ref);
         m = top;
-        l = l * was + lane_group_sum<64>(first + lane < parts ? w * ml.y : 0.f);
+        l = l * was + lane_group_sum<64>(w * ml.y);
 #pragma unroll
         for (int i = 0; i < CPL; ++i) acc[i] *= was;
-        const float* rows = c.ws + c.off_part + part * D + lane * CPL;
         const int here = min(parts - first, 64);
+        int s = 0;
+        if (first == 0) {
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e)
+                if (e < here) {
+                    const float ws = __shfl(w, e);
+#pragma unroll
+                    for (int i = 0; i < CPL; ++i) acc[i] += ws * ahead[e][i];
+                }
+            s = AHEAD;
+        }
 #pragma unroll 8
-        for (int s = 0; s < here; ++s) {
+        for (; s < here; ++s) {
             const float ws = __shfl(w, s);
 #pragma unroll
-            for (int i = 0; i < CPL; ++i) acc[i] += ws * rows[(size_t)s * N * D + i];
+            for (int i = 0; i < CPL; ++i) acc[i] += ws * rows[(size_t)(first + s) * N * D + i];
         }
     }
     const bool none = n == 0 && sees == 0;
     if (lane == 0 && c.lse != nullptr) c.lse[at] = none ? -INFINITY : (m + log2f(l)) * LN2;
-    float o_nla[CPL], o_la[CPL];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) {
         o_nla[i] = none ? 0.f : acc[i] / l;
-        o_la[i] = c.ws[c.off_ola + at * D + lane * CPL + i];
         res[i] = o_la[i] + o_nla[i];
     }
     if (c.combine_mode != 0) {
@@ -114,33 +150,44 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
     store(res);
 }
 
-// ---- commit: a block per output head; LPR = D / 4 lanes hold a row of S as a float4 each, the rows of S are independent of one
-// another, so that the path's tokens follow each other without a barrier ----
-constexpr int COMMIT_THREADS = 256;
+// ---- commit ----------------------------------------------------------------------------------------------------------------------
+// A block per output head.  Eight lanes hold a row of S (D / 8 elements each), and the rows are independent of one another, so that the path's
+// tokens follow each other without a barrier; eight tokens at a time come through LDS.  The state is kept as S / G with G the product
+// of the decays so far: a softmax token then costs nothing and a linear one two operations per element, the product with k and
+// the update (S would take a third).  G is taken back into S where it leaves 2^-40 .. 2^40.
+constexpr int COMMIT_THREADS = 256, COMMIT_TOKENS = 8;
 
 template <typename T, int D>
 __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitCall c) {
-    constexpr int LPR = D / 4, PER_PASS = COMMIT_THREADS / LPR, PASSES = D / PER_PASS;
+    constexpr int LPR = 8, PER_PASS = COMMIT_THREADS / LPR, PASSES = D / PER_PASS, W = D / 32;   // W: 4 elements each of a lane's share
+    __shared__ float s_k[COMMIT_TOKENS][D], s_v[COMMIT_TOKENS][D];
     __shared__ int s_path[64], s_row[64];
     __shared__ float s_a[64], s_b[64];
     __shared__ int s_n;
     const int bhg = blockIdx.x, bh = bhg / c.G, b = bh / c.H, tid = threadIdx.x, N = c.T;
-    const int node = c.node[b];
-    const bool refused = node < -1 || node >= N;
+    const int lr = tid % LPR, r0 = tid / LPR;
+    float* Sb = c.state + (size_t)bhg * D * D;
+    f32x4 S[PASSES][W];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int x = 0; x < W; ++x) S[p][x] = *reinterpret_cast<const f32x4*>(Sb + (size_t)(p * PER_PASS + r0) * D + 32 * x + 4 * lr);
     if (tid < 64) {
-        const bool none = refused || node < 0;
+        const int node = c.node[b];
+        const bool refused = node < -1 || node >= N, none = refused || node < 0;
+        const bool softmax = c.mask[(size_t)bh * N + min(tid, N - 1)] != 0;
+        const float alpha = c.alpha[(size_t)bh * N + min(tid, N - 1)], beta = c.beta[(size_t)bh * N + min(tid, N - 1)];
+        const int len = c.cache_len[bhg], had = min(max(len, 0), c.cap), room = len < 0 ? 0 : c.cap - had;
         const uint64_t anc = shfl_u64(ancestors(parent_of(c.parent, b, N, tid), tid), none ? 0 : node), path = none ? 0 : anc;
-        const bool on = (path >> tid) & 1;
-        const bool soft = on && c.mask[(size_t)bh * N + tid] != 0;
+        const bool on = (path >> tid) & 1, soft = on && softmax;
         const uint64_t softs = __ballot(soft);
         const uint64_t upto = (2ull << tid) - 1;        // lanes 0 .. tid (lane 63: all)
-        const int len = c.cache_len[bhg], had = min(max(len, 0), c.cap), room = len < 0 ? 0 : c.cap - had;
         const int rank = __popcll(softs & upto), stored = min(__popcll(softs), room);
         if (on) {
             const int p = __popcll(path & (upto >> 1));
             s_path[p] = tid;
-            s_a[p] = soft && c.freeze ? 1.f : c.alpha[(size_t)bh * N + tid];
-            s_b[p] = soft ? 0.f : c.beta[(size_t)bh * N + tid];
+            s_a[p] = soft && c.freeze ? 1.f : alpha;
+            s_b[p] = soft ? 0.f : beta;
             s_row[p] = soft && rank <= room ? had + rank - 1 : -1;
         }
         if (c.vis != nullptr && tid < N) c.vis[(size_t)bhg * N + tid] = on ? had + min(rank, room) : 0;
@@ -153,38 +200,59 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
     __syncthreads();
     const int n = s_n;
     if (n == 0) return;
-    const int lr = tid % LPR, r0 = tid / LPR;
-    float* Sb = c.state + (size_t)bhg * D * D;
     const T* k = (const T*)c.k + (size_t)bh * N * D;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : k;
     const T* v = (const T*)c.v + (size_t)bhg * N * D;
-    float4 S[PASSES];
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) S[p] = *reinterpret_cast<const float4*>(Sb + (size_t)(p * PER_PASS + r0) * D + lr * 4);
-    for (int i = 0; i < n; ++i) {
-        const int t = s_path[i], row = s_row[i];
-        const float a = s_a[i], bt = s_b[i];
-        float kk[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) kk[j] = to_float(k[t * D + lr * 4 + j]);
-#pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            float4 s = S[p];
-            s.x *= a; s.y *= a; s.z *= a; s.w *= a;
-            if (bt != 0.f) {
-                const float pred = lane_group_sum<LPR>(s.x * kk[0] + s.y * kk[1] + s.z * kk[2] + s.w * kk[3]);
-                const float delta = bt * (to_float(v[t * D + p * PER_PASS + r0]) - (c.linear_op == 0 ? pred : 0.f));
-                s.x += delta * kk[0]; s.y += delta * kk[1]; s.z += delta * kk[2]; s.w += delta * kk[3];
+    float G = 1.f;
+    for (int first = 0; first < n; first += COMMIT_TOKENS) {
+        const int here = min(n - first, COMMIT_TOKENS);
+        if (first > 0) __syncthreads();   // the tokens before have been used
+        for (int e = tid; e < here * D; e += COMMIT_THREADS) {
+            const int i = e / D, x = e % D, t = s_path[first + i], row = s_row[first + i];
+            const T vx = v[t * D + x];
+            s_k[i][x] = to_float(k[t * D + x]);
+            s_v[i][x] = to_float(vx);
+            if (row >= 0) {
+                ((T*)c.k_cache)[((size_t)bhg * c.cap + row) * D + x] = ks[t * D + x];
+                ((T*)c.v_cache)[((size_t)bhg * c.cap + row) * D + x] = vx;
             }
-            S[p] = s;
         }
-        if (row >= 0 && tid < D) {
-            ((T*)c.k_cache)[((size_t)bhg * c.cap + row) * D + tid] = ks[t * D + tid];
-            ((T*)c.v_cache)[((size_t)bhg * c.cap + row) * D + tid] = v[t * D + tid];
+        __syncthreads();
+        for (int i = 0; i < here; ++i) {
+            const float bt = s_b[first + i];
+            G *= s_a[first + i];
+            if (!(fabsf(G) > 0x1p-40f && fabsf(G) < 0x1p40f)) {
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+                    for (int x = 0; x < W; ++x) S[p][x] *= G;
+                G = 1.f;
+            }
+            if (bt == 0.f) continue;
+            f32x4 kk[W];
+#pragma unroll
+            for (int x = 0; x < W; ++x) kk[x] = *reinterpret_cast<const f32x4*>(&s_k[i][32 * x + 4 * lr]);
+            const float inv = 1.f / G;
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                float u = s_v[i][p * PER_PASS + r0];
+                if (c.linear_op == 0) {
+                    float pred = 0.f;
+#pragma unroll
+                    for (int x = 0; x < W; ++x)
+                        pred += S[p][x][0] * kk[x][0] + S[p][x][1] * kk[x][1] + S[p][x][2] * kk[x][2] + S[p][x][3] * kk[x][3];
+                    u -= G * lane_group_sum<LPR>(pred);
+                }
+                u *= bt * inv;
+#pragma unroll
+                for (int x = 0; x < W; ++x) S[p][x] += u * kk[x];
+            }
         }
     }
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) *reinterpret_cast<float4*>(Sb + (size_t)(p * PER_PASS + r0) * D + lr * 4) = S[p];
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int x = 0; x < W; ++x) *reinterpret_cast<f32x4*>(Sb + (size_t)(p * PER_PASS + r0) * D + 32 * x + 4 * lr) = G * S[p][x];
 }
 
 // ---- host side ----

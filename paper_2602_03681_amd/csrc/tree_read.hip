@@ -339,12 +339,14 @@ static void run_tree_read(const TreeCall& c, hipStream_t st) {
     else hipLaunchKernelGGL((tree_read_kernel<T, D, 2, 2, TURNS>), grid, block, 0, st, c);
 }
 
-// Rows of a part: as many as keep the partial results (4 T d bytes each, written and read) small beside the rows (4 d or 8 d bytes
-// each), unless there are too few parts to fill the chip.
+// Rows of a part.  Large parts make few partial results (4 T d bytes each, written and read) and long runs of rows; small ones fill the chip
+// where there are few caches, and even out their lengths.  us of both kernels with parts of 256 / 512 / 1024 / 2048 rows: 1024 caches of
+// 64 .. 2048 rows, 16 nodes 207 / 187 / 176 / 171; 32 of 32000, 64 nodes 227 / 176 / 154 / 140; 96 of 64 .. 1024, 33 nodes 36 / 34 / 41 /
+// 41; 16 of 1000, 16 nodes 17 / 18 / 24 / 23 (128 rows: 19).
 int tree_cache_rows(const TreeCall& c) {
     const long long heads = (long long)c.B * c.H * c.G;
-    int rows = 1024;
-    while (rows > 128 && heads * ((c.cap + rows - 1) / rows) < 2048) rows /= 2;
+    int rows = 2048;
+    while (rows > 256 && heads * ((c.cap + rows - 1) / rows) < (rows > 512 ? 512 : 192)) rows /= 2;
     return rows;
 }
 
