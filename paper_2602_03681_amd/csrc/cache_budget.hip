@@ -34,11 +34,19 @@ struct Rows16<bf16_t, D> {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
     }
-    __device__ __forceinline__ static f32x4 product(const Rows16& a, const Rows16& b) {
-        f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void load(const bf16_t* p, int l16, int lq, int pitch) {   // from LDS
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) s = mfma_bf16(a.x[i], b.x[i], s);
-        return s;
+        for (int i = 0; i < D / 32; ++i) x[i] = *reinterpret_cast<const u32x4*>(p + l16 * pitch + 32 * i + 8 * lq);
+    }
+    // with each of several (the sums side by side: an instruction does not wait for the one before)
+    template <int N>
+    __device__ __forceinline__ static void products(const Rows16& a, const Rows16 (&b)[N], f32x4 (&s)[N]) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = mfma_bf16(a.x[i], b[n].x[i], s[n]);
     }
 };
 template <int D>
@@ -49,11 +57,25 @@ struct Rows16<float, D> {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) x[i] = ld4(p + 16 * i);
     }
-    __device__ __forceinline__ static f32x4 product(const Rows16& a, const Rows16& b) {
-        f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void load(const float* p, int l16, int lq, int pitch) {   // from LDS
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) s = mac16(a.x[i], b.x[i], s);
-        return s;
+        for (int i = 0; i < D / 16; ++i) x[i] = ld4(p + l16 * pitch + 16 * i + 4 * lq);
+    }
+    template <int N>
+    __device__ __forceinline__ static void products(const Rows16& a, const Rows16 (&b)[N], f32x4 (&s)[N]) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].x, b[n].x[i].x, s[n], 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].y, b[n].x[i].y, s[n], 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].z, b[n].x[i].z, s[n], 0, 0, 0);
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i].w, b[n].x[i].w, s[n], 0, 0, 0);
+        }
     }
 };
 
@@ -103,11 +125,9 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_sums_kernel(WeightsCall
     }
     const float scale2 = c.scale * LOG2E;
     for (; row <= last; row += CW_WAVES * 16 * KT) {
-        f32x4 s[NQ][KT];
+        f32x4 s[KT][NQ];
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) s[x][i] = Rows16<T, D>::product(k[i], q[x]);
+        for (int i = 0; i < KT; ++i) Rows16<T, D>::products(k[i], q, s[i]);
 #pragma unroll
         for (int i = 0; i < KT; ++i) k[i].load(K, row + CW_WAVES * 16 * KT + 16 * i, last, l16, lq);
 #pragma unroll
@@ -118,8 +138,8 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_sums_kernel(WeightsCall
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r = row + 16 * i + 4 * lq + j;
-                    s[x][i][j] = r <= last && r < vis[x] ? s[x][i][j] * scale2 : -INFINITY;
-                    top = fmaxf(top, s[x][i][j]);
+                    s[i][x][j] = r <= last && r < vis[x] ? s[i][x][j] * scale2 : -INFINITY;
+                    top = fmaxf(top, s[i][x][j]);
                 }
             const float ref = top == -INFINITY ? 0.f : top;
             l[x] *= __builtin_amdgcn_exp2f(m[x] - ref);
@@ -127,12 +147,12 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_sums_kernel(WeightsCall
 #pragma unroll
             for (int i = 0; i < KT; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) l[x] += __builtin_amdgcn_exp2f(s[x][i][j] - ref);
+                for (int j = 0; j < 4; ++j) l[x] += __builtin_amdgcn_exp2f(s[i][x][j] - ref);
             if (KEEP && l16 < c.T) {
 #pragma unroll
                 for (int i = 0; i < KT; ++i)   // (rows past the end within the part have their place, too)
                     if (row + 16 * i + 4 * lq <= last)
-                        *reinterpret_cast<f32x4*>(c.ws + c.off_logits + ((size_t)bh * c.T + l16) * c.pitch + lo + row + 16 * i + 4 * lq) = s[x][i];
+                        *reinterpret_cast<f32x4*>(c.ws + c.off_logits + ((size_t)bh * c.T + l16) * c.pitch + lo + row + 16 * i + 4 * lq) = s[i][x];
             }
         }
     }
@@ -235,13 +255,13 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall 
     const float scale2 = c.scale * LOG2E;
     for (; row <= last; row += CW_WAVES * 16 * KT) {
         float sum[KT], w[KT];
-        f32x4 s[KT][NQ];
+        f32x4 s[NQ][KT];
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             w[i] = weights[min(row + 16 * i + l16, last)];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) s[i][x] = Rows16<T, D>::product(q[x], k[i]);
         }
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) Rows16<T, D>::products(q[x], k, s[x]);
 #pragma unroll
         for (int i = 0; i < KT; ++i) k[i].load(K, row + CW_WAVES * 16 * KT + 16 * i, last, l16, lq);
 #pragma unroll
@@ -252,7 +272,7 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall 
             for (int x = 0; x < NQ; ++x)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(s[i][x][j] * scale2 - L[x][j]);
+                    const float p = __builtin_amdgcn_exp2f(s[x][i][j] * scale2 - L[x][j]);
                     sum[i] += lo + r < vis[x][j] ? p : 0.f;
                 }
             sum[i] += lane_xor16(sum[i], lane);
@@ -263,9 +283,11 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall 
 }
 
 // ---- many queries: 16 KT rows stay in every wavefront's registers, the queries stream ----
-// WK of the block's wavefronts take rows side by side and the same queries, the others other queries: one wavefront's tile of queries is in the
-// CU's cache for the next.  Bounds of the block's queries (at most CW_CHUNK) go through LDS first; the tiles before the first one that
-// sees a row of the block's are left out.  Two tiles of queries are in registers: one is on its way while the other is multiplied.
+// WK of the block's wavefronts take rows side by side, the others other queries.  The queries come through LDS, 16 KB at a time and two steps
+// deep: read from memory by the wavefronts as operands, 16 rows apart from lane to lane, every lane is an access of its own to the CU's
+// cache, and their number (57 per instruction; 16 where four lanes read 64 bytes in a row) bound this kernel: 53 us against
+// the 34 of this form (a prompt of 8192, 32 caches of 410 rows).  Bounds of the block's queries (at most CW_CHUNK) go through LDS, too; the steps
+// before the first query that sees a row of the block's are left out.
 constexpr int CW_CHUNK = 1024;
 template <typename T, int D>
 constexpr int many_tiles() { return sizeof(T) == 2 || D == 64 ? 4 : 2; }
@@ -273,6 +295,11 @@ constexpr int many_tiles() { return sizeof(T) == 2 || D == 64 ? 4 : 2; }
 template <typename T, int D, int WK>
 __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall c) {
     constexpr int KT = many_tiles<T, D>(), WQ = CW_WAVES / WK, ROWS = 16 * KT * WK;
+    constexpr int QS = 16384 / (D * (int)sizeof(T));              // queries of a step: 32, 64 or 128
+    constexpr int LANES = D * (int)sizeof(T) / 16;                // 16-byte words of a row
+    constexpr int PITCH = D + LDS_PAD * 2 / (int)sizeof(T);       // elements
+    constexpr int WORDS = 16384 / 16 / CW_THREADS;                // per thread and step
+    __shared__ __attribute__((aligned(16))) T s_q[2][QS * PITCH];
     __shared__ float s_L[CW_CHUNK], s_sum[WQ][ROWS];
     __shared__ int s_vis[CW_CHUNK], s_first;
     const int bh = blockIdx.x, split = blockIdx.z, tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lq = lane >> 4;
@@ -286,7 +313,7 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall
     if (tid == 0) s_first = here;
     __syncthreads();
     int first = here;
-    for (int t = tid; t < (here + 15) / 16 * 16; t += CW_THREADS) {
+    for (int t = tid; t < (here + QS - 1) / QS * QS; t += CW_THREADS) {
         const int at = min(t, here - 1);
         const float x = lse[at];
         // queries that are not there, or whose lse is -inf, see nothing
@@ -298,36 +325,56 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall
     first = wave_extreme_i32<false>(first);
     if (lane == 0) atomicMin(&s_first, first);
     __syncthreads();
-    first = s_first / 16 * 16;
+    first = s_first / QS * QS;
+    if (first >= here) {   // (uniform)
+        if (tid < ROWS && block0 + tid < n) sums[block0 + tid] = 0.f;
+        return;
+    }
     float sum[KT];
 #pragma unroll
     for (int i = 0; i < KT; ++i) sum[i] = 0.f;
-    if (first < here && r0 < n) {
-        const float scale2 = c.scale * LOG2E;
-        Rows16<T, D> k[KT], q[2];
-        int t = first + 16 * wq;
+    const float scale2 = c.scale * LOG2E;
+    Rows16<T, D> k[KT];
+    u32x4 word[WORDS];
+    auto fetch = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < KT; ++i) k[i].load((const T*)c.k_cache + (size_t)bh * c.cap * D, r0 + 16 * i, n - 1, l16, lq);
-        q[0].load(Q, t, here - 1, l16, lq);
-        q[1].load(Q, t + 16 * WQ, here - 1, l16, lq);
-        while (t < here) {
+        for (int i = 0; i < WORDS; ++i) {
+            const int row = min(t + (tid + i * CW_THREADS) / LANES, here - 1);
+            word[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(Q + (size_t)row * D) + (tid % LANES) * 16);
+        }
+    };
+    auto put = [&](int at) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int at = min(t, (here - 1) / 16 * 16) + 4 * lq;   // (past the end: the last tile, which then counts for nothing)
-                const f32x4 L = *reinterpret_cast<const f32x4*>(&s_L[at]);
-                const int4 vis = *reinterpret_cast<const int4*>(&s_vis[at]);
+        for (int i = 0; i < WORDS; ++i)
+            *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&s_q[at][(tid + i * CW_THREADS) / LANES * PITCH]) + (tid % LANES) * 16) = word[i];
+    };
+    static_assert(CW_THREADS % LANES == 0 && QS % (16 * WQ) == 0, "a thread's words lie in one column, a step has a tile for every wavefront");
+    fetch(first);
+#pragma unroll
+    for (int i = 0; i < KT; ++i) k[i].load((const T*)c.k_cache + (size_t)bh * c.cap * D, r0 + 16 * i, n - 1, l16, lq);
+    put(0);
+    __syncthreads();
+    int at = 0;
+    for (int t = first; t < here; t += QS, at ^= 1) {
+        fetch(t + QS);   // (past the end: the last query)
+        if (r0 < n) {
+#pragma unroll
+            for (int x = 0; x < QS / (16 * WQ); ++x) {
+                const int u = 16 * (x * WQ + wq);
+                const f32x4 L = *reinterpret_cast<const f32x4*>(&s_L[t + u + 4 * lq]);
+                const int4 vis = *reinterpret_cast<const int4*>(&s_vis[t + u + 4 * lq]);
                 const int least = min(min(vis.x, vis.y), min(vis.z, vis.w)), most = max(max(vis.x, vis.y), max(vis.z, vis.w));
-                const bool any = t < here && __any(most > r0), all = __all(least >= r0 + 16 * KT);
+                if (!__any(most > r0)) continue;
+                Rows16<T, D> q;
+                q.load(&s_q[at][u * PITCH], l16, lq, PITCH);
                 f32x4 s[KT];
-#pragma unroll
-                for (int i = 0; i < KT; ++i) s[i] = Rows16<T, D>::product(q[u], k[i]);
-                q[u].load(Q, t + 32 * WQ, here - 1, l16, lq);
-                if (any && all) {
+                Rows16<T, D>::products(q, k, s);
+                if (__all(least >= r0 + 16 * KT)) {
 #pragma unroll
                     for (int i = 0; i < KT; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) sum[i] += __builtin_amdgcn_exp2f(s[i][j] * scale2 - L[j]);
-                } else if (any) {
+                } else {
                     const int v[4] = {vis.x, vis.y, vis.z, vis.w};
 #pragma unroll
                     for (int i = 0; i < KT; ++i)
@@ -337,9 +384,10 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall
                             sum[i] += r0 + 16 * i + l16 < v[j] ? p : 0.f;
                         }
                 }
-                t += 16 * WQ;
             }
         }
+        put(at ^ 1);     // (its queries were used up before the barrier)
+        __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
@@ -360,6 +408,7 @@ __global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c)
     const int bh = blockIdx.x, r = blockIdx.y * CW_THREADS + threadIdx.x;
     if (r >= rows_of(c, bh)) return;
     float x = 0.f;
+#pragma unroll 8
     for (int s = 0; s < c.splits; ++s) x += c.ws[c.off_sums + ((size_t)s * c.B * c.H + bh) * c.cap + r];
     float* w = c.weights + (size_t)bh * c.cap + r;
     *w = c.decay * *w + x;
@@ -386,12 +435,17 @@ size_t weights_workspace(WeightsCall& c, bool lse_given) {
         }
     }
     if (c.T > CW_FEW) {
-        // rows of a block: those of up to four wavefronts, as the caches have them; queries: as many as leave enough blocks
-        const int tiles = 16 * (c.dtype == NATS_BF16 || c.d == 64 ? 4 : 2);
-        c.row_waves = c.cap <= tiles ? 1 : c.cap <= 2 * tiles ? 2 : 4;
-        const long long blocks = heads * ((c.cap + c.row_waves * tiles - 1) / (c.row_waves * tiles));
+        // rows of a block: those of up to four wavefronts, as the caches have them, for every row of the block's shares the reading of its
+        // queries; queries of a block: as many as leave four blocks per CU.  Fewer rows, too, where that leaves the chip idle
+        // (us of the kernel with 4 / 2 / 1 wavefronts on the rows: 32 caches of 410 rows, 8192 queries, 512 at a time 34 / 37 / 46;
+        // 6 caches of 105 rows in fp32, 701 queries, 128 at a time 12 / 8 / 6).
+        const int tiles = 16 * (c.dtype == NATS_BF16 || c.d == 64 ? 4 : 2), least = c.dtype == NATS_F32 && c.d == 128 ? 2 : 1;
+        auto blocks = [&] { return heads * ((c.cap + c.row_waves * tiles - 1) / (c.row_waves * tiles)) * ((c.T + c.chunk - 1) / c.chunk); };
+        c.row_waves = c.cap <= tiles ? least : c.cap <= 2 * tiles ? 2 : 4;
         c.chunk = CW_CHUNK;
-        while (c.chunk > 128 && blocks * ((c.T + c.chunk - 1) / c.chunk) < 2048) c.chunk /= 2;
+        while (c.chunk > 128 && blocks() < 1024) c.chunk /= 2;
+        while (c.row_waves > least && blocks() < 256) c.row_waves /= 2;
+        if (blocks() < 256) c.chunk = 64;
         c.splits = (c.T + c.chunk - 1) / c.chunk;
         c.off_sums = at;
         at += (size_t)c.splits * heads * c.cap;
@@ -440,9 +494,10 @@ static nats_status run_weights(const WeightsCall& c, hipStream_t st) {
         ProfScope ps("weights_many", st);
         constexpr int ROWS = 16 * many_tiles<T, D>();
         const dim3 grid(heads, (c.cap + c.row_waves * ROWS - 1) / (c.row_waves * ROWS), c.splits);
-        if (c.row_waves == 1) hipLaunchKernelGGL((weights_many_kernel<T, D, 1>), grid, block, 0, st, c);
-        else if (c.row_waves == 2) hipLaunchKernelGGL((weights_many_kernel<T, D, 2>), grid, block, 0, st, c);
-        else hipLaunchKernelGGL((weights_many_kernel<T, D, 4>), grid, block, 0, st, c);
+        if constexpr (ROWS > 32)   // (16 KB of longer rows are too few queries for four wavefronts)
+            if (c.row_waves == 1) hipLaunchKernelGGL((weights_many_kernel<T, D, 1>), grid, block, 0, st, c);
+        if (c.row_waves == 2) hipLaunchKernelGGL((weights_many_kernel<T, D, 2>), grid, block, 0, st, c);
+        if (c.row_waves == 4) hipLaunchKernelGGL((weights_many_kernel<T, D, 4>), grid, block, 0, st, c);
     }
     ProfScope ps("weights_join", st);
     hipLaunchKernelGGL(weights_join_kernel, rows, block, 0, st, c);

@@ -236,3 +236,29 @@ def test_prompt_drafts_weights_and_eviction_together(dtype):
         kept = nats.cache_evict(t["k_cache"], t["v_cache"], t["cache_len"], weights, keep, 10)
         for name, got in (("k_cache", t["k_cache"]), ("v_cache", t["v_cache"]), ("cache_len", t["cache_len"]), ("weights", weights), ("kept", kept)):
             assert torch.equal(got.cpu(), want[name]), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [1, 16, 20, 33, 64, 70, 129, 260, 530])
+@pytest.mark.parametrize("T", [65, 200])
+def test_many_queries_over_caches_of_every_width(dtype, d, cap, T):
+    """Every number of wavefronts side by side on the rows, queries in one step and in several."""
+    x = inputs(1, 3, T, d, cap, DT[dtype], seed=cap + T)
+    g = torch.Generator().manual_seed(cap)
+    vis = torch.randint(0, cap + 1, (1, 3, T), generator=g, dtype=torch.int32).sort(-1).values
+    vis[:, :, -1] = cap
+    x["cache_len"][0, 0] = cap
+    check(x, vis=vis)
+    _, lse = ref.cache_weights(**x, vis=vis)
+    check(x, vis=vis, lse=lse.float())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_heads_and_queries(dtype):
+    """Enough blocks that the queries go 256 and more at a time, several steps to a block."""
+    x = inputs(2, 16, 1500, 64, 300, DT[dtype], seed=77)
+    g = torch.Generator().manual_seed(77)
+    vis = torch.randint(0, 301, (2, 16, 1500), generator=g, dtype=torch.int32).sort(-1).values
+    _, lse = ref.cache_weights(**x, vis=vis)
+    check(x, vis=vis, lse=lse.float(), decay=0.5)
