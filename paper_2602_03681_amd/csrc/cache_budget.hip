@@ -184,39 +184,37 @@ __global__ __launch_bounds__(CW_THREADS) void weights_lse_kernel(WeightsCall c) 
     c.ws[c.off_lse + (size_t)bh * c.T + t] = l == 0.f ? -INFINITY : (m + log2f(l)) / LOG2E;
 }
 
-// ---- the weights from logits that were kept: a thread per row ----
+// ---- the weights from logits that were kept ----
+constexpr int CW_KEPT_ROWS = 4;   // per thread
 __global__ __launch_bounds__(CW_THREADS) void weights_kept_kernel(WeightsCall c) {
-    __shared__ float s_m[CW_THREADS], s_l[CW_THREADS], s_lse[CW_KEEP];
-    const int bh = blockIdx.x, tid = threadIdx.x, r = blockIdx.y * CW_THREADS + tid, n = rows_of(c, bh);
-    if ((int)blockIdx.y * CW_THREADS >= n) return;
-    const float* z = c.ws + c.off_logits + (size_t)bh * c.T * c.pitch + r;
-    float x[CW_KEEP], w = 0.f;
-#pragma unroll
-    for (int t = 0; t < CW_KEEP; ++t) x[t] = t < c.T && r < n ? z[(size_t)t * c.pitch] : -INFINITY;
-    if (r < n) w = c.decay * c.weights[(size_t)bh * c.cap + r];
-    {   // the parts of query tid % 16, sixteen threads to a query
-        const int t = tid % CW_KEEP, parts = (n + c.rows - 1) / c.rows;
-        float m = -INFINITY, l = 0.f;
-        for (int p = tid / CW_KEEP; t < c.T && p < parts; p += CW_THREADS / CW_KEEP) {
-            const float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (((size_t)bh * c.parts + p) * c.T + t) * 2);
-            join(m, l, ml.x, ml.y);
-        }
-        s_m[tid] = m;
-        s_l[tid] = l;
+    const int bh = blockIdx.x, lane = threadIdx.x & 63, n = rows_of(c, bh), r0 = blockIdx.y * CW_THREADS * CW_KEPT_ROWS + threadIdx.x;
+    if ((int)blockIdx.y * CW_THREADS * CW_KEPT_ROWS >= n) return;
+    const float* z = c.ws + c.off_logits + (size_t)bh * c.T * c.pitch;
+    float* weights = c.weights + (size_t)bh * c.cap;
+    // the parts' sums of query lane % 16, a quarter of the parts per lane, by every wavefront for itself
+    const int t = min(lane % CW_KEEP, c.T - 1), parts = (n + c.rows - 1) / c.rows;
+    float m = -INFINITY, l = 0.f, w[CW_KEPT_ROWS], sum[CW_KEPT_ROWS];
+    for (int p = lane / CW_KEEP; p < parts; p += 64 / CW_KEEP) {
+        const float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (((size_t)bh * c.parts + p) * c.T + t) * 2);
+        join(m, l, ml.x, ml.y);
     }
-    __syncthreads();
-    if (tid < CW_KEEP) {
-        float m = s_m[tid], l = s_l[tid];
-        for (int i = 1; i < CW_THREADS / CW_KEEP; ++i) join(m, l, s_m[i * CW_KEEP + tid], s_l[i * CW_KEEP + tid]);
-        s_lse[tid] = l == 0.f ? INFINITY : m + log2f(l);   // a query that sees nothing: all its logits are -inf
-    }
-    __syncthreads();
-    if (r >= n) return;
-    float sum = 0.f;
 #pragma unroll
-    for (int t = 0; t < CW_KEEP; ++t)
-        if (t < c.T) sum += __builtin_amdgcn_exp2f(x[t] - s_lse[t]);
-    c.weights[(size_t)bh * c.cap + r] = w + sum;
+    for (int i = 0; i < CW_KEPT_ROWS; ++i) {
+        w[i] = weights[min(r0 + i * CW_THREADS, n - 1)];
+        sum[i] = 0.f;
+    }
+    join(m, l, lane_xor16(m, lane), lane_xor16(l, lane));
+    join(m, l, lane_xor32(m, lane), lane_xor32(l, lane));
+    const float lse = l == 0.f ? INFINITY : m + log2f(l);   // (a query that sees nothing: all its logits are -inf)
+#pragma unroll 4
+    for (int q = 0; q < c.T; ++q) {
+        const float L = __shfl(lse, q);
+#pragma unroll
+        for (int i = 0; i < CW_KEPT_ROWS; ++i) sum[i] += __builtin_amdgcn_exp2f(z[(size_t)q * c.pitch + min(r0 + i * CW_THREADS, n - 1)] - L);
+    }
+#pragma unroll
+    for (int i = 0; i < CW_KEPT_ROWS; ++i)
+        if (r0 + i * CW_THREADS < n) weights[r0 + i * CW_THREADS] = c.decay * w[i] + sum[i];
 }
 
 // lse in powers of two and the number of visible rows of queries t .. t + 3 (those beyond T see nothing, nor do those with lse -inf)
@@ -477,7 +475,8 @@ static nats_status run_weights(const WeightsCall& c, hipStream_t st) {
         }
         if (c.T <= CW_KEEP) {
             ProfScope ps("weights_kept", st);
-            hipLaunchKernelGGL(weights_kept_kernel, rows, block, 0, st, c);
+            constexpr int ROWS = CW_THREADS * CW_KEPT_ROWS;
+            hipLaunchKernelGGL(weights_kept_kernel, dim3(heads, (c.cap + ROWS - 1) / ROWS), block, 0, st, c);
             return check_launch("cache_weights");
         }
         ProfScope ps("weights_lse", st);

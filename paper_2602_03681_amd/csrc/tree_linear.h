@@ -59,10 +59,29 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
     const int row0 = 16 * (part * TURNS * TL_WAVES + wave);   // of the wavefront's first turn
     load_state(row0);
 
+    // ---- N and P, the products: the lower triangle's tiles, dealt out to the wavefronts; the first tile's rows are asked for before the
+    // last two wavefronts, which have the fewest tiles, look at the tree ----
+    auto load_nodes = [&](const T* x, int tile, Raw8<T> (&r)[KS]) {
+        const T* p = x + (size_t)min(16 * tile + l16, N - 1) * D + 8 * lq;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) r[i].load(p + 32 * i);
+    };
+    constexpr int PAIRS = NT * (NT + 1) / 2, PER_WAVE = (PAIRS + TL_WAVES - 1) / TL_WAVES;
+    auto tile_row = [](int pair) { return pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3; };
+    f32x4 kk[PER_WAVE], qk[PER_WAVE];
+    Raw8<T> ki[KS], qi[KS], kj[KS];
+    auto load_pair = [&](int pair) {
+        const int ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
+        load_nodes(k, ti, ki);
+        load_nodes(q, ti, qi);
+        load_nodes(k, tj, kj);
+    };
+    load_pair(min(wave, PAIRS - 1));
+
     // ---- paths (one wavefront), their decays (another) ----
-    if (wave < 2) {
+    if (wave >= TL_WAVES - 2) {
         const int par = parent_of(c.parent, b, N, lane);
-        if (wave == 0) {
+        if (wave == TL_WAVES - 1) {
             const uint64_t anc = ancestors(par, lane);
             s.anc[lane] = anc;
             s.par[lane] = par;
@@ -92,25 +111,11 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         }
     }
 
-    // ---- N and P: the lower triangle's tiles, dealt out to the wavefronts ----
-    auto load_nodes = [&](const T* x, int tile, Raw8<T> (&r)[KS]) {
-        const T* p = x + (size_t)min(16 * tile + l16, N - 1) * D + 8 * lq;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) r[i].load(p + 32 * i);
-    };
-    constexpr int PAIRS = NT * (NT + 1) / 2, PER_WAVE = (PAIRS + TL_WAVES - 1) / TL_WAVES;
-    f32x4 kk[PER_WAVE], qk[PER_WAVE];
 #pragma unroll
     for (int x = 0; x < PER_WAVE; ++x) {
-        const int pair = wave + x * TL_WAVES;
-        if (pair >= PAIRS) break;
-        const int ti = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, tj = pair - ti * (ti + 1) / 2;
         kk[x] = qk[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (16 * ti >= N) continue;
-        Raw8<T> ki[KS], qi[KS], kj[KS];
-        load_nodes(k, ti, ki);
-        load_nodes(q, ti, qi);
-        load_nodes(k, tj, kj);
+        if (wave + x * TL_WAVES >= PAIRS) break;
+        if (x > 0) load_pair(wave + x * TL_WAVES);
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
             u32x4 tk[terms_of<T>()], tq[terms_of<T>()], tb[terms_of<T>()];
@@ -127,7 +132,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
     for (int x = 0; x < PER_WAVE; ++x) {
         const int pair = wave + x * TL_WAVES;
         if (pair >= PAIRS) break;
-        const int ti = pair < 1 ? 0 : pair < 3 ? 1 : pair < 6 ? 2 : 3, tj = pair - ti * (ti + 1) / 2;
+        const int ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
         const int j = 16 * tj + l16;
         const double lgj = s.lg[j];
 #pragma unroll
@@ -146,7 +151,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         }
     }
     __syncthreads();
-    // ---- the diagonal blocks' inverses: lane (tile, column) ----
+    // ---- the diagonal blocks' inverses: lane (tile, column); the first K S^T and Q S^T are done beside them ----
     if (wave == 0 && lane < 16 * NT && c.linear_op == 0) {
         float x[16];
 #pragma unroll
@@ -158,14 +163,8 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
             s.inv[lq][i][l16] = sum;
         }
     }
-    __syncthreads();
-
-    // ---- 16 columns at a time ----
-    float* O = c.ws + c.off_ola + (size_t)bhg * N * D;
-#pragma unroll
-    for (int turn = 0; turn < TURNS; ++turn) {
-        const int col = row0 + 16 * TL_WAVES * turn + l16;
-        f32x4 w[NT], o[NT];
+    f32x4 w[NT], o[NT];
+    auto state_products = [&] {
 #pragma unroll
         for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -185,6 +184,16 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 o[t] = mfma_terms(tx, ts, o[t]);
             }
         }
+    };
+    state_products();
+    __syncthreads();
+
+    // ---- 16 columns at a time ----
+    float* O = c.ws + c.off_ola + (size_t)bhg * N * D;
+#pragma unroll
+    for (int turn = 0; turn < TURNS; ++turn) {
+        const int col = row0 + 16 * TL_WAVES * turn + l16;
+        if (turn > 0) state_products();
         if (turn + 1 < TURNS) load_state(row0 + 16 * TL_WAVES * (turn + 1));
         f32x4 u[NT];
         bool fine = true;

@@ -314,16 +314,17 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
 
 static_assert(TC_THREADS == TL_THREADS, "blocks of either kind in one launch");
 
-template <typename T, int D, int NQ, int QG, int TURNS>
+template <typename T, int D, int NT, int TURNS>
 __global__ __launch_bounds__(TC_THREADS, 2) void tree_read_kernel(TreeCall c) {
     constexpr int PARTS = D / (64 * TURNS);   // blocks of a head's linear branch
+    constexpr int NQ = NT == 1 ? 1 : 2, QG = NT <= 2 ? 1 : 2;
     __shared__ union {
-        LinearLds<NQ * QG> linear;
+        LinearLds<NT> linear;
         CacheLds<D, NQ> cache;
     } s;
     const int heads = c.B * c.H * c.G, id = blockIdx.x;
     if (id < heads * PARTS) {
-        tree_linear_block<T, D, NQ * QG, TURNS>(c, id / PARTS, id % PARTS, s.linear);
+        tree_linear_block<T, D, NT, TURNS>(c, id / PARTS, id % PARTS, s.linear);
     } else {
         const int x = id - heads * PARTS;
         tree_cache_block<T, D, NQ, QG>(c, x / c.n_split, x % c.n_split, s.cache);
@@ -334,9 +335,10 @@ template <typename T, int D, int TURNS>
 static void run_tree_read(const TreeCall& c, hipStream_t st) {
     const int heads = c.B * c.H * c.G;
     const dim3 grid(heads * (D / (64 * TURNS)) + heads * c.n_split), block(TC_THREADS);
-    if (c.T <= 16) hipLaunchKernelGGL((tree_read_kernel<T, D, 1, 1, TURNS>), grid, block, 0, st, c);
-    else if (c.T <= 32) hipLaunchKernelGGL((tree_read_kernel<T, D, 2, 1, TURNS>), grid, block, 0, st, c);
-    else hipLaunchKernelGGL((tree_read_kernel<T, D, 2, 2, TURNS>), grid, block, 0, st, c);
+    if (c.T <= 16) hipLaunchKernelGGL((tree_read_kernel<T, D, 1, TURNS>), grid, block, 0, st, c);
+    else if (c.T <= 32) hipLaunchKernelGGL((tree_read_kernel<T, D, 2, TURNS>), grid, block, 0, st, c);
+    else if (c.T <= 48) hipLaunchKernelGGL((tree_read_kernel<T, D, 3, TURNS>), grid, block, 0, st, c);
+    else hipLaunchKernelGGL((tree_read_kernel<T, D, 4, TURNS>), grid, block, 0, st, c);
 }
 
 // Rows of a part.  Large parts make few partial results (4 T d bytes each, written and read) and long runs of rows; small ones fill the chip
