@@ -509,25 +509,27 @@ nats_status launch_cache_weights(const WeightsCall& c, hipStream_t st) {
 }
 
 // ---- eviction: which rows stay ---------------------------------------------------------------------------------------------
-// A number that orders as the weights do (a NaN below all, -0 as 0)
+// A number that orders as the weights do (a NaN below all, -0 as 0); 0 is left for what is not to be chosen
 __device__ __forceinline__ uint32_t weight_key(float w) {
-    if (w != w) return 0;
+    if (w != w) return 1;
     const uint32_t u = __float_as_uint(w + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
 // One block per cache.  The weight of the last row that stays is found digit by digit: 8 bits of its key at a time, from counts of the
-// rows that agree in the digits so far.  Then the rows above it, the lowest of those equal to it and the last `recent` ones are
-// numbered in order, and their weights moved.  The counts are kept in four copies, a lane's by its number: the first digit of attention weights
-// takes a dozen values, and lanes that add to one address go one after the other.  A wavefront has PER x 64 rows in a row, so that ranks inside it are counts of ballot bits.
-// Up to THREADS x PER rows the weights stay in registers throughout; longer caches are gone through in such steps, once per digit
-// and once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its old one).
+// rows that agree in the digits so far.  The counts are kept in four copies, a lane's by its number: the first digit of attention weights
+// takes a dozen values, and lanes that add to one address go one after the other.  As soon as few enough rows agree, their keys go
+// into LDS and the other rows are left alone.  Then the rows above the weight found and the lowest of those equal to it are numbered in
+// order and their weights moved, behind them the last `recent` ones.  A wavefront has PER x 64 rows in a row, so that ranks inside it are
+// counts of ballot bits.  Up to THREADS x PER rows the keys stay in registers throughout; longer caches are gone through in such steps,
+// once per digit and once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its
+// old one).  With few caches it is bound by its instructions, on the few CUs that have one: about 30 per row and lane.
 template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
-    constexpr int WAVES = THREADS / 64, STEP = THREADS * PER;
+    constexpr int WAVES = THREADS / 64, STEP = THREADS * PER, FEW = 8 * THREADS;
     __shared__ int4 s_hist[256];   // copy lane % 4 of every count
-    __shared__ int s_ties[WAVES], s_stay[WAVES], s_rest;
-    __shared__ uint32_t s_digit;
+    __shared__ uint32_t s_few[FEW], s_digit;
+    __shared__ int s_ties[WAVES], s_stay[WAVES], s_rest, s_agree, s_n;
     const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = min(max(c.cache_len[bh], 0), c.cap);
     float* w = c.weights + (size_t)bh * c.cap;
@@ -536,30 +538,48 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
         for (int r = tid; r < c.keep; r += THREADS) kept[r] = r < n ? r : -1;
         return;
     }
-    const int m = n - c.recent;     // the rows to choose from
-    int rest = c.keep - c.recent;   // of those that agree with `prefix`, this many stay
-    const bool any = rest > 0, one = n <= STEP;
-    const int first = wave * 64 * PER + lane;
-    float x[PER];
+    const int m = n - c.recent;                       // the rows to choose from
+    const int chosen = c.keep - c.recent;             // ... and how many of them stay
+    const bool one = m <= STEP;
+    uint32_t key[PER];
     auto load = [&](int r0) {
+        const int first = r0 + wave * 64 * PER;       // uniform
+        const float* x = w + first;
+        if (first + 64 * PER <= m) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int r = r0 + first + 64 * i;
-            x[i] = r < n ? w[r] : 0.f;
+            for (int i = 0; i < PER; ++i) key[i] = weight_key(x[(uint32_t)lane + 64u * i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int r = first + lane + 64 * i;
+                const uint32_t k = weight_key(w[(uint32_t)min(r, n - 1)]);
+                key[i] = r < m ? k : 0;
+            }
         }
     };
     if (one) load(0);
     uint32_t prefix = 0;
-    for (int shift = 24; any && shift >= 0; shift -= 8) {
+    int rest = chosen;   // of the rows that agree with `prefix`, this many stay
+    int few = -1;        // keys in LDS
+    auto count = [&](uint32_t k, int shift) { atomicAdd(reinterpret_cast<int*>(&s_hist[(k >> shift) & 255]) + (lane & 3), 1); };
+    for (int shift = 24; chosen > 0 && shift >= 0; shift -= 8) {
+        const int above = shift + 8;
         for (int i = tid; i < 256; i += THREADS) s_hist[i] = make_int4(0, 0, 0, 0);
         __syncthreads();
-        for (int r0 = 0; r0 < m; r0 += STEP) {
-            if (!one) load(r0);
+        if (few >= 0) {
+            for (int i = tid; i < few; i += THREADS)
+                if ((s_few[i] >> above) == (prefix >> above)) count(s_few[i], shift);
+        } else {
+            for (int r0 = 0; r0 < m; r0 += STEP) {
+                if (!one) load(r0);
+                if (shift == 24) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t key = weight_key(x[i]);
-                if (r0 + first + 64 * i < m && (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))))
-                    atomicAdd(reinterpret_cast<int*>(&s_hist[(key >> shift) & 255]) + (lane & 3), 1);
+                    for (int i = 0; i < PER; ++i) count(key[i], 24);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if ((key[i] >> above) == (prefix >> above)) count(key[i], shift);
+                }
             }
         }
         __syncthreads();
@@ -570,30 +590,38 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
                 const int4 x = s_hist[255 - 4 * lane - i];
                 sum += h[i] = x.x + x.y + x.z + x.w;
             }
-            int above = wave_inclusive_scan_i32(sum) - sum;
-            if (above < rest && rest <= above + sum) {
+            int more = wave_inclusive_scan_i32(sum) - sum;
+            if (more < rest && rest <= more + sum) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (above < rest && rest <= above + h[i]) {
+                    if (more < rest && rest <= more + h[i]) {
                         s_digit = 255 - 4 * lane - i;
-                        s_rest = rest - above;
+                        s_rest = rest - more;
+                        s_agree = h[i];
                     }
-                    above += h[i];
+                    more += h[i];
                 }
             }
+            if (lane == 0) s_n = 0;
         }
         __syncthreads();
         prefix |= s_digit << shift;
         rest = s_rest;
+        if (one && few < 0 && shift > 0 && s_agree <= FEW) {   // (in any order: they are only counted)
+            few = s_agree;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if ((key[i] >> shift) == (prefix >> shift)) s_few[atomicAdd(&s_n, 1)] = key[i];
+        }
     }
+    // (keys that stay are `prefix` at least, and more than 0: the rows that are not to be chosen do not reach it)
     int done = 0, equal = 0;   // rows that stay, and rows equal to the last weight that stays, of the steps before
-    const uint64_t below = (1ull << lane) - 1;
-    for (int r0 = 0; r0 < n; r0 += STEP) {
+    auto before = [&](uint64_t b) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0)); };
+    for (int r0 = 0; chosen > 0 && r0 < m; r0 += STEP) {
         if (!one) load(r0);
-        auto ties = [&](int i) { return any && r0 + first + 64 * i < m && weight_key(x[i]) == prefix; };
         int n_ties = 0, n_stay = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) n_ties += __popcll(__ballot(ties(i)));
+        for (int i = 0; i < PER; ++i) n_ties += __popcll(__ballot(key[i] == prefix));
         if (lane == 0) s_ties[wave] = n_ties;
         __syncthreads();
         int rank = equal;
@@ -602,19 +630,26 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
             if (v < wave) rank += s_ties[v];
             equal += s_ties[v];
         }
+        const float* mine = w + r0 + wave * 64 * PER;
         uint32_t stays = 0;
+        float x[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int r = r0 + first + 64 * i;
-            const bool tie = ties(i);
-            const uint64_t b = __ballot(tie);
-            const bool stay = r < n && (r >= m || (any && (weight_key(x[i]) > prefix || (tie && rank + __popcll(b & below) < rest))));
-            rank += __popcll(b);
+            bool stay = key[i] > prefix;
+            const uint64_t b = __ballot(key[i] == prefix);
+            if (b != 0) {   // (uniform)
+                stay = stay || (key[i] == prefix && rank + before(b) < rest);
+                rank += __popcll(b);
+            }
             stays |= stay ? 1u << i : 0u;
             n_stay += __popcll(__ballot(stay));
+            if (stay) x[i] = mine[(uint32_t)lane + 64u * i];
+            else x[i] = 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(x[i]));   // every weight of the step has arrived before the barrier
         if (lane == 0) s_stay[wave] = n_stay;
-        __syncthreads();   // (every weight of the step has been read)
+        __syncthreads();
         int at = done;
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) {
@@ -626,11 +661,23 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
             const bool stay = (stays >> i) & 1;
             const uint64_t b = __ballot(stay);
             if (stay) {
-                const int to = at + __popcll(b & below);
+                const uint32_t to = (uint32_t)(at + before(b));
                 w[to] = x[i];
-                kept[to] = r0 + first + 64 * i;
+                kept[to] = r0 + wave * 64 * PER + lane + 64 * i;
             }
             at += __popcll(b);
+        }
+    }
+    // the last rows, from m on to `chosen` on
+    for (int i0 = 0; i0 < c.recent; i0 += THREADS) {
+        const int i = i0 + tid;
+        float x = 0.f;
+        if (i < c.recent) x = w[m + i];
+        asm volatile("" : "+v"(x));
+        __syncthreads();   // (the chosen rows' weights were read before, and so were this step's)
+        if (i < c.recent) {
+            w[chosen + i] = x;
+            kept[chosen + i] = m + i;
         }
     }
     if (tid == 0) c.cache_len[bh] = c.keep;
@@ -693,7 +740,8 @@ nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
         else hipLaunchKernelGGL((evict_select_kernel<1024, 32>), dim3(heads), dim3(1024), 0, st, c);
     }
     ProfScope ps("evict_move", st);
-    // slices as wide as leave two blocks per CU; where even narrow ones do not, blocks of 1024 threads
+    // slices as wide as leave two blocks per CU; where even 64 bytes do not, blocks of 1024 threads, and 32 bytes below one (16 caches of
+    // 32000 rows to 8192: 35 us, 41 with 64 bytes, 47 with 256 threads)
     auto move = [&](auto slice, auto threads) {
         constexpr int SLICE = decltype(slice)::value, THREADS = decltype(threads)::value;
         hipLaunchKernelGGL((evict_move_kernel<SLICE, THREADS>), dim3(heads, 2 * (row_bytes / SLICE)), dim3(THREADS), 0, st, c, row_bytes);
@@ -703,7 +751,8 @@ nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
     if (row_bytes >= 256 && bytes >= 512 * 256) move(integral_constant<int, 256>{}, integral_constant<int, 256>{});
     else if (bytes >= 512 * 128) move(integral_constant<int, 128>{}, integral_constant<int, 256>{});
     else if (bytes >= 512 * 64) move(integral_constant<int, 64>{}, integral_constant<int, 256>{});
-    else move(integral_constant<int, 64>{}, integral_constant<int, 1024>{});
+    else if (bytes >= 256 * 64) move(integral_constant<int, 64>{}, integral_constant<int, 1024>{});
+    else move(integral_constant<int, 32>{}, integral_constant<int, 1024>{});
     return check_launch("cache_evict");
 }
 

@@ -262,3 +262,13 @@ def test_many_heads_and_queries(dtype):
     vis = torch.randint(0, 301, (2, 16, 1500), generator=g, dtype=torch.int32).sort(-1).values
     _, lse = ref.cache_weights(**x, vis=vis)
     check(x, vis=vis, lse=lse.float(), decay=0.5)
+
+
+def test_evict_from_a_cache_of_several_steps():
+    """More rows than a block keeps in its registers; many equal weights, so that ranks go on from step to step."""
+    k, v, n, w = evict_inputs(1, 2, 64, 70000, torch.bfloat16, seed=6, lens=69999)
+    check_evict(k, v, n, w, 40000, 1500)
+    check_evict(k, v, n, (w * 3).floor(), 50000, 0)
+    check_evict(k, v, n, w, 33000, 33000)
+    n[0, 1] = 32769
+    check_evict(k, v, n, (w * 3).floor(), 300, 10)
