@@ -524,19 +524,24 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // counts of ballot bits.  Up to THREADS x PER rows the keys stay in registers throughout; longer caches are gone through in such steps,
 // once per digit and once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its
 // old one).  With few caches it is bound by its instructions, on the few CUs that have one: about 30 per row and lane.
+template <int THREADS>
+struct SelectLds {
+    int4 hist[256];   // copy lane % 4 of every count
+    uint32_t few[8 * THREADS], digit;
+    int ties[THREADS / 64], stay[THREADS / 64], rest, agree, n;
+};
+
+// false: the cache is within the budget, no row moves
 template <int THREADS, int PER>
-__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
+__device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectLds<THREADS>& s) {
     constexpr int WAVES = THREADS / 64, STEP = THREADS * PER, FEW = 8 * THREADS;
-    __shared__ int4 s_hist[256];   // copy lane % 4 of every count
-    __shared__ uint32_t s_few[FEW], s_digit;
-    __shared__ int s_ties[WAVES], s_stay[WAVES], s_rest, s_agree, s_n;
-    const int bh = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = min(max(c.cache_len[bh], 0), c.cap);
     float* w = c.weights + (size_t)bh * c.cap;
     int32_t* kept = c.kept + (size_t)bh * c.keep;
     if (n <= c.keep) {
         for (int r = tid; r < c.keep; r += THREADS) kept[r] = r < n ? r : -1;
-        return;
+        return false;
     }
     const int m = n - c.recent;                       // the rows to choose from
     const int chosen = c.keep - c.recent;             // ... and how many of them stay
@@ -561,14 +566,14 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
     uint32_t prefix = 0;
     int rest = chosen;   // of the rows that agree with `prefix`, this many stay
     int few = -1;        // keys in LDS
-    auto count = [&](uint32_t k, int shift) { atomicAdd(reinterpret_cast<int*>(&s_hist[(k >> shift) & 255]) + (lane & 3), 1); };
+    auto count = [&](uint32_t k, int shift) { atomicAdd(reinterpret_cast<int*>(&s.hist[(k >> shift) & 255]) + (lane & 3), 1); };
     for (int shift = 24; chosen > 0 && shift >= 0; shift -= 8) {
         const int above = shift + 8;
-        for (int i = tid; i < 256; i += THREADS) s_hist[i] = make_int4(0, 0, 0, 0);
+        for (int i = tid; i < 256; i += THREADS) s.hist[i] = make_int4(0, 0, 0, 0);
         __syncthreads();
         if (few >= 0) {
             for (int i = tid; i < few; i += THREADS)
-                if ((s_few[i] >> above) == (prefix >> above)) count(s_few[i], shift);
+                if ((s.few[i] >> above) == (prefix >> above)) count(s.few[i], shift);
         } else {
             for (int r0 = 0; r0 < m; r0 += STEP) {
                 if (!one) load(r0);
@@ -587,7 +592,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
             int h[4], sum = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int4 x = s_hist[255 - 4 * lane - i];
+                const int4 x = s.hist[255 - 4 * lane - i];
                 sum += h[i] = x.x + x.y + x.z + x.w;
             }
             int more = wave_inclusive_scan_i32(sum) - sum;
@@ -595,23 +600,23 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (more < rest && rest <= more + h[i]) {
-                        s_digit = 255 - 4 * lane - i;
-                        s_rest = rest - more;
-                        s_agree = h[i];
+                        s.digit = 255 - 4 * lane - i;
+                        s.rest = rest - more;
+                        s.agree = h[i];
                     }
                     more += h[i];
                 }
             }
-            if (lane == 0) s_n = 0;
+            if (lane == 0) s.n = 0;
         }
         __syncthreads();
-        prefix |= s_digit << shift;
-        rest = s_rest;
-        if (one && few < 0 && shift > 0 && s_agree <= FEW) {   // (in any order: they are only counted)
-            few = s_agree;
+        prefix |= s.digit << shift;
+        rest = s.rest;
+        if (one && few < 0 && shift > 0 && s.agree <= FEW) {   // (in any order: they are only counted)
+            few = s.agree;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                if ((key[i] >> shift) == (prefix >> shift)) s_few[atomicAdd(&s_n, 1)] = key[i];
+                if ((key[i] >> shift) == (prefix >> shift)) s.few[atomicAdd(&s.n, 1)] = key[i];
         }
     }
     // (keys that stay are `prefix` at least, and more than 0: the rows that are not to be chosen do not reach it)
@@ -622,13 +627,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
         int n_ties = 0, n_stay = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) n_ties += __popcll(__ballot(key[i] == prefix));
-        if (lane == 0) s_ties[wave] = n_ties;
+        if (lane == 0) s.ties[wave] = n_ties;
         __syncthreads();
         int rank = equal;
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) {
-            if (v < wave) rank += s_ties[v];
-            equal += s_ties[v];
+            if (v < wave) rank += s.ties[v];
+            equal += s.ties[v];
         }
         const float* mine = w + r0 + wave * 64 * PER;
         uint32_t stays = 0;
@@ -648,13 +653,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(x[i]));   // every weight of the step has arrived before the barrier
-        if (lane == 0) s_stay[wave] = n_stay;
+        if (lane == 0) s.stay[wave] = n_stay;
         __syncthreads();
         int at = done;
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) {
-            if (v < wave) at += s_stay[v];
-            done += s_stay[v];
+            if (v < wave) at += s.stay[v];
+            done += s.stay[v];
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -681,6 +686,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
         }
     }
     if (tid == 0) c.cache_len[bh] = c.keep;
+    return true;
+}
+
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
+    __shared__ SelectLds<THREADS> s;
+    evict_select<THREADS, PER>(c, blockIdx.x, s);
 }
 
 // ---- eviction: the rows move ---------------------------------------------------------------------------------------------------
@@ -689,24 +701,21 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictCall c) {
 // step's, which lie behind all that this one writes, are on their way meanwhile.
 constexpr int MV_WORDS = 8;   // 16-byte words per thread and step
 template <int SLICE, int THREADS>
-__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int row_bytes) {
+__device__ __forceinline__ void evict_move_rows(const int32_t* kept, int keep, char* rows, int row_bytes) {
     constexpr int LANES = SLICE / 16, PER_WORD = THREADS / LANES, STEP = PER_WORD * MV_WORDS;   // rows
-    const int bh = blockIdx.x, slices = row_bytes / SLICE, tid = threadIdx.x;
-    const int array = blockIdx.y / slices, slice = blockIdx.y % slices;
-    char* base = (char*)(array == 0 ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + slice * SLICE + (tid % LANES) * 16;
-    const int32_t* kept = c.kept + (size_t)bh * c.keep;
-    const int mine = tid / LANES;
+    const int tid = threadIdx.x, mine = tid / LANES;
+    char* base = rows + (tid % LANES) * 16;
     uint4 now[MV_WORDS], next[MV_WORDS];
     int src[MV_WORDS], src_next[MV_WORDS];
     auto sources = [&](int r0, int (&s)[MV_WORDS]) {
 #pragma unroll
         for (int i = 0; i < MV_WORDS; ++i) {
             const int r = r0 + mine + i * PER_WORD;
-            s[i] = kept[min(r, c.keep - 1)];
-            s[i] = r < c.keep && s[i] > r ? s[i] : -1;   // (a row that stays where it is is not touched)
+            s[i] = kept[min(r, keep - 1)];
+            s[i] = r < keep && s[i] > r ? s[i] : -1;   // (a row that stays where it is is not touched)
         }
     };
-    auto rows = [&](const int (&s)[MV_WORDS], uint4 (&x)[MV_WORDS]) {
+    auto fetch = [&](const int (&s)[MV_WORDS], uint4 (&x)[MV_WORDS]) {
 #pragma unroll
         for (int i = 0; i < MV_WORDS; ++i) {
             x[i] = make_uint4(0, 0, 0, 0);
@@ -714,10 +723,10 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int ro
         }
     };
     sources(0, src);
-    rows(src, now);
+    fetch(src, now);
     sources(STEP, src_next);
-    for (int r0 = 0; r0 < c.keep; r0 += STEP) {
-        rows(src_next, next);
+    for (int r0 = 0; r0 < keep; r0 += STEP) {
+        fetch(src_next, next);
 #pragma unroll
         for (int i = 0; i < MV_WORDS; ++i) asm volatile("" : "+v"(now[i].x), "+v"(now[i].y), "+v"(now[i].z), "+v"(now[i].w));   // they are here
         __syncthreads();
@@ -731,12 +740,46 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int ro
     }
 }
 
+template <int SLICE, int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int row_bytes) {
+    const int bh = blockIdx.x, slices = row_bytes / SLICE, array = blockIdx.y / slices, slice = blockIdx.y % slices;
+    evict_move_rows<SLICE, THREADS>(c.kept + (size_t)bh * c.keep, c.keep,
+                                    (char*)(array == 0 ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + slice * SLICE, row_bytes);
+}
+
+// Both by one block per cache: where there are caches enough to fill the chip, one cache's selection hides behind another's rows (1024 caches
+// of 700 .. 2048 rows to 1024: 167 us + 13 us as two launches), and where there is little to move a launch is most of the time.
+template <int THREADS, int PER, int ROW>
+__global__ __launch_bounds__(THREADS, 4) void evict_kernel(EvictCall c) {
+    __shared__ SelectLds<THREADS> s;
+    const int bh = blockIdx.x;
+    if (!evict_select<THREADS, PER>(c, bh, s)) return;
+    __syncthreads();   // `kept` is there
+    const size_t at = (size_t)bh * c.cap * ROW;
+    evict_move_rows<ROW, THREADS>(c.kept + (size_t)bh * c.keep, c.keep, (char*)c.k_cache + at, ROW);
+    evict_move_rows<ROW, THREADS>(c.kept + (size_t)bh * c.keep, c.keep, (char*)c.v_cache + at, ROW);
+}
+
 nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
+    using std::integral_constant;
     const int heads = c.B * c.H, row_bytes = c.d * (c.dtype == NATS_F32 ? 4 : 2);
+    if (c.cap <= 4096 && (heads >= 256 || (long long)c.keep * row_bytes <= 128 << 10)) {
+        ProfScope ps("evict", st);
+        auto run = [&](auto per, auto row) {
+            hipLaunchKernelGGL((evict_kernel<256, decltype(per)::value, decltype(row)::value>), dim3(heads), dim3(256), 0, st, c);
+        };
+        auto rows = [&](auto per) {
+            if (row_bytes == 128) run(per, integral_constant<int, 128>{});
+            else if (row_bytes == 256) run(per, integral_constant<int, 256>{});
+            else run(per, integral_constant<int, 512>{});
+        };
+        if (c.cap <= 1024) rows(integral_constant<int, 4>{});
+        else rows(integral_constant<int, 16>{});
+        return check_launch("cache_evict");
+    }
     {
         ProfScope ps("evict_select", st);
-        if (c.cap <= 1024) hipLaunchKernelGGL((evict_select_kernel<256, 4>), dim3(heads), dim3(256), 0, st, c);
-        else if (c.cap <= 4096) hipLaunchKernelGGL((evict_select_kernel<256, 16>), dim3(heads), dim3(256), 0, st, c);
+        if (c.cap <= 4096) hipLaunchKernelGGL((evict_select_kernel<256, 16>), dim3(heads), dim3(256), 0, st, c);
         else hipLaunchKernelGGL((evict_select_kernel<1024, 32>), dim3(heads), dim3(1024), 0, st, c);
     }
     ProfScope ps("evict_move", st);
@@ -746,7 +789,6 @@ nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
         constexpr int SLICE = decltype(slice)::value, THREADS = decltype(threads)::value;
         hipLaunchKernelGGL((evict_move_kernel<SLICE, THREADS>), dim3(heads, 2 * (row_bytes / SLICE)), dim3(THREADS), 0, st, c, row_bytes);
     };
-    using std::integral_constant;
     const int bytes = heads * 2 * row_bytes;   // of a row of all caches, K and V
     if (row_bytes >= 256 && bytes >= 512 * 256) move(integral_constant<int, 256>{}, integral_constant<int, 256>{});
     else if (bytes >= 512 * 128) move(integral_constant<int, 128>{}, integral_constant<int, 256>{});
