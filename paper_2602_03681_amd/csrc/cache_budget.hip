@@ -412,11 +412,12 @@ __global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c)
     *w = c.decay * *w + x;
 }
 
-// Rows of a part: enough parts to fill the chip, where there are rows for that.
+// Rows of a part: as many as leave two parts per CU, at most 512 (us with parts of 128 / 256 / 512 / 1024 / 2048 rows: 1024 caches of 64 .. 2048 rows,
+// one query 74 / 69 / 69 / 72 / 77; 140 of up to 2778 rows, 64 queries 34 / 25 / 24 / 25 / 34).
 size_t weights_workspace(WeightsCall& c, bool lse_given) {
     const long long heads = (long long)c.B * c.H;
-    c.rows = 1024;
-    while (c.rows > 128 && heads * ((c.cap + c.rows - 1) / c.rows) < 2048) c.rows /= 2;
+    c.rows = 512;
+    while (c.rows > 128 && heads * ((c.cap + c.rows - 1) / c.rows) < 512) c.rows /= 2;
     c.parts = (c.cap + c.rows - 1) / c.rows;
     size_t at = 0;
     if (!lse_given) {
