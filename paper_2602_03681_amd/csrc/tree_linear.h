@@ -58,6 +58,14 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
     };
     const int row0 = 16 * (part * TURNS * TL_WAVES + wave);   // of the wavefront's first turn
     load_state(row0);
+    float vv[NT][4];
+    auto load_values = [&](int col) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vv[t][e] = to_float(v[(size_t)min(16 * t + 4 * lq + e, N - 1) * D + col]);
+    };
+    load_values(row0 + l16);
 
     // ---- N and P, the products: the lower triangle's tiles, dealt out to the wavefronts; the first tile's rows are asked for before the
     // last two wavefronts, which have the fewest tiles, look at the tree ----
@@ -193,7 +201,10 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
 #pragma unroll
     for (int turn = 0; turn < TURNS; ++turn) {
         const int col = row0 + 16 * TL_WAVES * turn + l16;
-        if (turn > 0) state_products();
+        if (turn > 0) {
+            load_values(col);
+            state_products();
+        }
         if (turn + 1 < TURNS) load_state(row0 + 16 * TL_WAVES * (turn + 1));
         f32x4 u[NT];
         bool fine = true;
@@ -202,8 +213,8 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
             const f32x4 g = *reinterpret_cast<const f32x4*>(&s.g[16 * t + 4 * lq]), bt = *reinterpret_cast<const f32x4*>(&s.b[16 * t + 4 * lq]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float x = to_float(v[(size_t)min(16 * t + 4 * lq + e, N - 1) * D + col]);
-                w[t][e] = bt[e] == 0.f ? 0.f : bt[e] * (c.linear_op == 0 ? x - g[e] * w[t][e] : x);
+                const float x = bt[e] * (c.linear_op == 0 ? vv[t][e] - g[e] * w[t][e] : vv[t][e]);
+                w[t][e] = bt[e] == 0.f ? 0.f : x;   // (a softmax token writes nothing, whatever its v)
                 o[t][e] *= g[e];
             }
             u[t] = w[t];
