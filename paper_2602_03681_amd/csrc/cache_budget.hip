@@ -412,12 +412,11 @@ __global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c)
     *w = c.decay * *w + x;
 }
 
-// Rows of a part: as many as leave two parts per CU, at most 512 (us with parts of 128 / 256 / 512 / 1024 / 2048 rows: 1024 caches of 64 .. 2048 rows,
-// one query 74 / 69 / 69 / 72 / 77; 140 of up to 2778 rows, 64 queries 34 / 25 / 24 / 25 / 34).
+// Rows of a part: 256, or 128 where that leaves less than two parts per CU (us with parts of 128 / 256 / 512 / 1024 rows: 1024 caches of 64 ..
+// 2048 rows, one query 74 / 69 / 69 / 72; 140 of up to 2778, 64 queries 34 / 25 / 24 / 25; 42 of up to 17187, 10 queries 21 / 20 / 24 / 27).
 size_t weights_workspace(WeightsCall& c, bool lse_given) {
     const long long heads = (long long)c.B * c.H;
-    c.rows = 512;
-    while (c.rows > 128 && heads * ((c.cap + c.rows - 1) / c.rows) < 512) c.rows /= 2;
+    c.rows = heads * ((c.cap + 255) / 256) < 512 ? 128 : 256;
     c.parts = (c.cap + c.rows - 1) / c.rows;
     size_t at = 0;
     if (!lse_given) {
@@ -567,6 +566,7 @@ __device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectL
     uint32_t prefix = 0;
     int rest = chosen;   // of the rows that agree with `prefix`, this many stay
     int few = -1;        // keys in LDS
+    auto before = [&](uint64_t b) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0)); };
     auto count = [&](uint32_t k, int shift) { atomicAdd(reinterpret_cast<int*>(&s.hist[(k >> shift) & 255]) + (lane & 3), 1); };
     for (int shift = 24; chosen > 0 && shift >= 0; shift -= 8) {
         const int above = shift + 8;
@@ -615,14 +615,22 @@ __device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectL
         rest = s.rest;
         if (one && few < 0 && shift > 0 && s.agree <= FEW) {   // (in any order: they are only counted)
             few = s.agree;
+            int mine = 0, at = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if ((key[i] >> shift) == (prefix >> shift)) s.few[atomicAdd(&s.n, 1)] = key[i];
+            for (int i = 0; i < PER; ++i) mine += __popcll(__ballot((key[i] >> shift) == (prefix >> shift)));
+            if (lane == 0) at = atomicAdd(&s.n, mine);
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const bool agrees = (key[i] >> shift) == (prefix >> shift);
+                const uint64_t b = __ballot(agrees);
+                if (agrees) s.few[at + before(b)] = key[i];
+                at += __popcll(b);
+            }
         }
     }
     // (keys that stay are `prefix` at least, and more than 0: the rows that are not to be chosen do not reach it)
     int done = 0, equal = 0;   // rows that stay, and rows equal to the last weight that stays, of the steps before
-    auto before = [&](uint64_t b) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0)); };
     for (int r0 = 0; chosen > 0 && r0 < m; r0 += STEP) {
         if (!one) load(r0);
         int n_ties = 0, n_stay = 0;
