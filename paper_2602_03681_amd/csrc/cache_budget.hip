@@ -287,6 +287,7 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_few_kernel(WeightsCall 
 // the 34 of this form (a prompt of 8192, 32 caches of 410 rows).  Bounds of the block's queries (at most CW_CHUNK) go through LDS, too; the steps
 // before the first query that sees a row of the block's are left out.
 constexpr int CW_CHUNK = 1024;
+constexpr int CW_SPLITS = 64;   // blocks that share a row's queries in one launch (each writes a sum per row)
 template <typename T, int D>
 constexpr int many_tiles() { return sizeof(T) == 2 || D == 64 ? 4 : 2; }
 
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % WK, wq = wave / WK;
     const int n = rows_of(c, bh), block0 = blockIdx.y * ROWS, r0 = block0 + wk * 16 * KT;
     if (block0 >= n) return;
-    const int t0 = split * c.chunk, here = min(c.chunk, c.T - t0);
+    const int t0 = c.t_lo + split * c.chunk, here = min(c.chunk, c.t_hi - t0);
     const T* Q = queries<T>(c, bh) + (size_t)t0 * D;
     const float* lse = (c.lse != nullptr ? c.lse : c.ws + c.off_lse) + (size_t)bh * c.T + t0;
     float* sums = c.ws + c.off_sums + ((size_t)split * c.B * c.H + bh) * c.cap;
@@ -401,15 +402,15 @@ __global__ __launch_bounds__(CW_THREADS, 2) void weights_many_kernel(WeightsCall
     sums[block0 + tid] = x;
 }
 
-// the splits' sums onto the weights, in order
-__global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c) {
+// the splits' sums onto the weights, in order; decay 1 for all but a call's first launch
+__global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c, int splits, float decay) {
     const int bh = blockIdx.x, r = blockIdx.y * CW_THREADS + threadIdx.x;
     if (r >= rows_of(c, bh)) return;
     float x = 0.f;
 #pragma unroll 8
-    for (int s = 0; s < c.splits; ++s) x += c.ws[c.off_sums + ((size_t)s * c.B * c.H + bh) * c.cap + r];
+    for (int s = 0; s < splits; ++s) x += c.ws[c.off_sums + ((size_t)s * c.B * c.H + bh) * c.cap + r];
     float* w = c.weights + (size_t)bh * c.cap + r;
-    *w = c.decay * *w + x;
+    *w = decay * *w + x;
 }
 
 // Rows of a part: 256, or 128 where that leaves less than two parts per CU (us with parts of 128 / 256 / 512 / 1024 rows: 1024 caches of 64 ..
@@ -444,7 +445,7 @@ size_t weights_workspace(WeightsCall& c, bool lse_given) {
         while (c.chunk > 128 && blocks() < 1024) c.chunk /= 2;
         while (c.row_waves > least && blocks() < 256) c.row_waves /= 2;
         if (blocks() < 256) c.chunk = 64;
-        c.splits = (c.T + c.chunk - 1) / c.chunk;
+        c.splits = min((c.T + c.chunk - 1) / c.chunk, CW_SPLITS);
         c.off_sums = at;
         at += (size_t)c.splits * heads * c.cap;
     }
@@ -489,17 +490,23 @@ static nats_status run_weights(const WeightsCall& c, hipStream_t st) {
         else hipLaunchKernelGGL((weights_few_kernel<T, D, 4>), dim3(heads, c.parts), block, 0, st, c);
         return check_launch("cache_weights");
     }
-    {
-        ProfScope ps("weights_many", st);
-        constexpr int ROWS = 16 * many_tiles<T, D>();
-        const dim3 grid(heads, (c.cap + c.row_waves * ROWS - 1) / (c.row_waves * ROWS), c.splits);
-        if constexpr (ROWS > 32)   // (16 KB of longer rows are too few queries for four wavefronts)
-            if (c.row_waves == 1) hipLaunchKernelGGL((weights_many_kernel<T, D, 1>), grid, block, 0, st, c);
-        if (c.row_waves == 2) hipLaunchKernelGGL((weights_many_kernel<T, D, 2>), grid, block, 0, st, c);
-        if (c.row_waves == 4) hipLaunchKernelGGL((weights_many_kernel<T, D, 4>), grid, block, 0, st, c);
+    constexpr int ROWS = 16 * many_tiles<T, D>();
+    for (int t = 0; t < c.T; t += c.splits * c.chunk) {
+        WeightsCall x = c;
+        x.t_lo = t;
+        x.t_hi = min(c.T - t, c.splits * c.chunk) + t;
+        const int splits = (x.t_hi - x.t_lo + c.chunk - 1) / c.chunk;
+        {
+            ProfScope ps("weights_many", st);
+            const dim3 grid(heads, (c.cap + c.row_waves * ROWS - 1) / (c.row_waves * ROWS), splits);
+            if constexpr (ROWS > 32)   // (16 KB of longer rows are too few queries for four wavefronts)
+                if (c.row_waves == 1) hipLaunchKernelGGL((weights_many_kernel<T, D, 1>), grid, block, 0, st, x);
+            if (c.row_waves == 2) hipLaunchKernelGGL((weights_many_kernel<T, D, 2>), grid, block, 0, st, x);
+            if (c.row_waves == 4) hipLaunchKernelGGL((weights_many_kernel<T, D, 4>), grid, block, 0, st, x);
+        }
+        ProfScope ps("weights_join", st);
+        hipLaunchKernelGGL(weights_join_kernel, rows, block, 0, st, x, splits, t == 0 ? c.decay : 1.f);
     }
-    ProfScope ps("weights_join", st);
-    hipLaunchKernelGGL(weights_join_kernel, rows, block, 0, st, c);
     return check_launch("cache_weights");
 }
 

@@ -1,4 +1,4 @@
-// Host path of the calls that are made once per generated token (and of the plain forward): checks, output allocation
+// Host path of the calls that are made once per generated token, or per round of drafted tokens: checks, output allocation
 // and the call into libnats.so without a trip through Python per argument.
 //
 // The kernels of a step at small batches take 6 to 8 us; checking fifteen tensors and filling a ctypes call in Python took 12.5

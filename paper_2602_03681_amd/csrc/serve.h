@@ -57,6 +57,7 @@ struct WeightsCall {
     int rows, parts;                                   // rows of a part, parts of a cache
     int row_waves, chunk, splits;                      // more than 64 queries: wavefronts of a block that take rows side by side, its
                                                        // queries, blocks that share a head's queries
+    int t_lo, t_hi;                                    // the queries of a launch
     int pitch;                                         // of the logits that are kept
     size_t off_ml, off_logits, off_lse, off_sums;      // floats
 };

@@ -272,3 +272,13 @@ def test_evict_from_a_cache_of_several_steps():
     check_evict(k, v, n, w, 33000, 33000)
     n[0, 1] = 32769
     check_evict(k, v, n, (w * 3).floor(), 300, 10)
+
+
+@pytest.mark.parametrize("T", [66000, 70001])
+def test_more_queries_than_a_block_takes_at_once(T):
+    x = inputs(1, 2, T, 64, 40, torch.bfloat16, seed=T, lens=40)
+    g = torch.Generator().manual_seed(T)
+    vis = torch.randint(0, 41, (1, 2, T), generator=g, dtype=torch.int32).sort(-1).values
+    _, lse = ref.cache_weights(**x, vis=vis)
+    # the sums of T terms: by lanes, wavefronts and blocks, none of more than 1100 terms in a row
+    check(x, vis=vis, lse=lse.float())
