@@ -22,14 +22,19 @@ struct TreeCall {
     void* o;
     float* lse;
     float* ws;
-    int rows, n_split;                          // rows of a part, parts of a cache
-    size_t off_anc, off_ola, off_part, off_ml;  // floats
+    // parts of the caches: `rows` rows each, n_split of a cache, or (even != 0) `even` blocks with the same number of rows each
+    int rows, n_split, even;
+    size_t off_anc, off_ola, off_part, off_ml, off_units;  // floats
+    // Even parts go by units of TREE_UNIT rows: units()[h] of them lie before cache h (all of them: h = heads), units()[heads + 1] make a
+    // block's share.  The part of cache h that block x has is part h + x of all.
+    __host__ __device__ int32_t* units() const { return reinterpret_cast<int32_t*>(ws + off_units); }
     // [B][T] ancestor sets, from the linear branch's blocks to the merge
     __host__ __device__ uint64_t* anc() const { return reinterpret_cast<uint64_t*>(ws + off_anc); }
 };
-size_t tree_workspace(TreeCall& c);    // floats; fills rows, n_split and the offsets
+constexpr int TREE_UNIT = 32;
+size_t tree_workspace(TreeCall& c);    // floats; fills rows, n_split, even and the offsets
 nats_status launch_tree(const TreeCall& c, hipStream_t st);
-int tree_cache_rows(const TreeCall& c);
+void tree_cache_parts(TreeCall& c);
 nats_status launch_tree_read(const TreeCall& c, hipStream_t st);   // both branches
 
 struct TreeCommitCall {

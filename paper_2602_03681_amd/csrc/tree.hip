@@ -40,20 +40,28 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
     constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
     const T* ks = c.k_nla != nullptr ? (const T*)c.k_nla + (size_t)bhg * N * D : (const T*)c.k + (size_t)bh * N * D;
     const T* v = (const T*)c.v + (size_t)bhg * N * D;
-    const size_t part0 = (size_t)bhg * c.n_split * N + t;
+    const int n = min(max(c.cache_len[bhg], 0), c.cap);
+    int slot0 = bhg * c.n_split, parts = (n + c.rows - 1) / c.rows, last = c.n_split - 1;
+    if (c.even) {
+        const int32_t* units = c.units();
+        const int from = units[bhg], to = units[bhg + 1], share = units[gridDim.y + 1];
+        slot0 = bhg + from / share;
+        parts = to > from ? (to - 1) / share - from / share + 1 : 0;
+        last = max(parts - 1, 0);
+    }
+    const size_t part0 = (size_t)slot0 * N + t;
     const float* rows = c.ws + c.off_part + part0 * D + lane * CPL;
     const uint64_t anc = c.anc()[(size_t)b * N + t];
     const bool is_soft = c.mask[(size_t)bh * N + min(lane, N - 1)] != 0;
     float q[CPL], ahead[AHEAD][CPL], o_nla[CPL], o_la[CPL];
     columns(c.q_nla != nullptr ? (const T*)c.q_nla + at * D : (const T*)c.q + ((size_t)bh * N + t) * D, q);
-    float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part0 + (size_t)min(lane, c.n_split - 1) * N) * 2);
+    float2 ml = *reinterpret_cast<const float2*>(c.ws + c.off_ml + (part0 + (size_t)min(lane, last) * N) * 2);
 #pragma unroll
     for (int s = 0; s < AHEAD; ++s)
 #pragma unroll
-        for (int i = 0; i < CPL; ++i) ahead[s][i] = rows[(size_t)min(s, c.n_split - 1) * N * D + i];
+        for (int i = 0; i < CPL; ++i) ahead[s][i] = rows[(size_t)min(s, last) * N * D + i];
 #pragma unroll
     for (int i = 0; i < CPL; ++i) o_la[i] = c.ws[c.off_ola + at * D + lane * CPL + i];
-    const int n = min(max(c.cache_len[bhg], 0), c.cap), parts = (n + c.rows - 1) / c.rows;
     const uint64_t sees = anc & __ballot(lane < N && is_soft);
 
     // the node's softmax ancestors, four at a time; logits in the parts' units (powers of 2), the same in every lane
@@ -258,13 +266,14 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
 // ---- host side ----
 size_t tree_workspace(TreeCall& c) {
     const size_t heads = (size_t)c.B * c.H * c.G;
-    c.rows = tree_cache_rows(c);
-    c.n_split = (c.cap + c.rows - 1) / c.rows;
+    tree_cache_parts(c);
+    const size_t parts = c.even ? heads + c.even : heads * c.n_split;
     c.off_anc = 0;
     c.off_ola = align_up((size_t)c.B * c.T * 2, 4);
     c.off_part = c.off_ola + heads * c.T * c.d;
-    c.off_ml = c.off_part + heads * c.n_split * c.T * c.d;
-    return c.off_ml + heads * c.n_split * c.T * 2;
+    c.off_ml = c.off_part + parts * c.T * c.d;
+    c.off_units = c.off_ml + parts * c.T * 2;
+    return c.off_units + (c.even ? heads + 2 : 0);
 }
 
 template <typename T, int D>

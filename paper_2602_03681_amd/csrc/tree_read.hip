@@ -62,12 +62,14 @@ struct CacheTile<bf16_t, D> {
             for (int i = 0; i < D / 32; ++i) k[t][i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
         }
     }
+    template <bool ONCE>   // (read by one wavefront alone, in whole lines: past the caches)
     __device__ __forceinline__ void load_v(const bf16_t* V, int row, int last, int l16, int lq) {
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             const bf16_t* p = V + (size_t)min(row + 16 * (s / 4) + 4 * lq + s % 4, last) * D + 2 * W * l16;
             if constexpr (W == 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+                const u32x4* w = reinterpret_cast<const u32x4*>(p);
+                const u32x4 x = ONCE ? __builtin_nontemporal_load(w) : *w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[s][i] = x[i];
             } else {
@@ -135,6 +137,7 @@ struct CacheTile<float, D> {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) k[i] = ld4(p + 16 * i);
     }
+    template <bool ONCE>
     __device__ __forceinline__ void load_v(const float* V, int row, int last, int l16, int lq) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -178,8 +181,9 @@ struct CacheTile<float, D> {
 };
 
 constexpr int TC_THREADS = 256, TC_WAVES = TC_THREADS / 64;
+constexpr int TREE_LEAST_UNITS = 8;   // of a block's share
 
-// NQ: tiles of 16 queries per wavefront; QG: groups of 16 NQ queries in a block, the block's other wavefronts share the rows
+// `count` rows of cache bhg from `lo` on, into part `slot`.  NQ: tiles of 16 queries per wavefront; QG: groups of 16 NQ queries in a block, the block's other wavefronts share the rows
 template <int D, int NQ>
 struct CacheLds {
     f32x4 o[2][NQ * (D / 16)][64];
@@ -187,7 +191,7 @@ struct CacheLds {
 };
 
 template <typename T, int D, int NQ, int QG>
-__device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int split, CacheLds<D, NQ>& lds) {
+__device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int lo, int count, int slot, CacheLds<D, NQ>& lds) {
     using Tile = CacheTile<T, D>;
     constexpr int KT = Tile::KT, ROWS = 16 * KT, KG = TC_WAVES / QG, E = D / 16;
     constexpr float LOG2E = 1.44269504088896341f;
@@ -195,8 +199,7 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
     auto& s_ml = lds.ml;
     const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = wave / KG, kg = wave % KG;
-    const int n = min(max(c.cache_len[bhg], 0), c.cap), lo = split * c.rows, last = min(n - lo, c.rows) - 1;
-    if (last < 0) return;   // uniform: the merge knows from the same length which parts exist
+    const int last = count - 1;
     const T* K = (const T*)c.k_cache + ((size_t)bhg * c.cap + lo) * D;
     const T* V = (const T*)c.v_cache + ((size_t)bhg * c.cap + lo) * D;
     const T* Q = c.q_nla != nullptr ? (const T*)c.q_nla + (size_t)bhg * c.T * D : (const T*)c.q + (size_t)(bhg / c.G) * c.T * D;
@@ -207,7 +210,7 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
     Tile tile;
     int row = kg * ROWS;
     tile.load_k(K, row, last, l16, lq);
-    tile.load_v(V, row, last, l16, lq);
+    tile.template load_v<QG == 1>(V, row, last, l16, lq);
     typename Tile::Query q[NQ];
     f32x4 o[NQ][E];
     float m[NQ], l[NQ];
@@ -262,7 +265,7 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
         }
         if (!whole) tile.clear_v(row, last, lq);
         tile.template products<NQ>(w, o);
-        tile.load_v(V, next, last, l16, lq);
+        tile.template load_v<QG == 1>(V, next, last, l16, lq);
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) l[i] = over_quads_sum(l[i]);
@@ -270,34 +273,34 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
     // the wavefronts that share queries: the upper half of them hands its result to the lower half, until one is left
 #pragma unroll
     for (int half = KG / 2; half >= 1; half /= 2) {
-        const int slot = qg * half + kg % half;
+        const int place = qg * half + kg % half;
         static_assert(QG * (KG / 2) <= 2, "slots");
         if (half < KG / 2) __syncthreads();   // the slots have been read
         if (kg >= half && kg < 2 * half) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                s_ml[slot][i][0][lane] = m[i];
-                s_ml[slot][i][1][lane] = l[i];
+                s_ml[place][i][0][lane] = m[i];
+                s_ml[place][i][1][lane] = l[i];
 #pragma unroll
-                for (int e = 0; e < E; ++e) s_o[slot][i * E + e][lane] = o[i][e];
+                for (int e = 0; e < E; ++e) s_o[place][i * E + e][lane] = o[i][e];
             }
         }
         __syncthreads();
         if (kg < half) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
-                const float m2 = s_ml[slot][i][0][lane], l2 = s_ml[slot][i][1][lane];
+                const float m2 = s_ml[place][i][0][lane], l2 = s_ml[place][i][1][lane];
                 const float top = fmaxf(m[i], m2), ref = top == -INFINITY ? 0.f : top;
                 const float w1 = __builtin_amdgcn_exp2f(m[i] - ref), w2 = __builtin_amdgcn_exp2f(m2 - ref);
                 m[i] = top;
                 l[i] = w1 * l[i] + w2 * l2;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[i][e] = w1 * o[i][e] + w2 * s_o[slot][i * E + e][lane];
+                for (int e = 0; e < E; ++e) o[i][e] = w1 * o[i][e] + w2 * s_o[place][i * E + e][lane];
             }
         }
     }
     if (kg != 0) return;
-    const size_t part = ((size_t)bhg * c.n_split + split) * c.T;
+    const size_t part = (size_t)slot * c.T;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const int t = (qg * NQ + i) * 16 + l16;
@@ -314,7 +317,60 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
 
 static_assert(TC_THREADS == TL_THREADS, "blocks of either kind in one launch");
 
-template <typename T, int D, int NT, int TURNS>
+// Block x of c.even: an equal share of the rows of all caches, which may begin and end inside one.
+template <typename T, int D, int NQ, int QG>
+__device__ __forceinline__ void tree_even_block(const TreeCall& c, int x, int heads, CacheLds<D, NQ>& lds) {
+    auto length = [&](int h) { return min(max(c.cache_len[h], 0), c.cap); };
+    // the caches' units counted by all threads, some caches in a row each
+    __shared__ int s_sum[TC_WAVES], s_head, s_unit;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (heads + TC_THREADS - 1) / TC_THREADS, first = min(tid * each, heads), end = min(first + each, heads);
+    auto units = [](int rows) { return (rows + TREE_UNIT - 1) / TREE_UNIT; };
+    int mine = 0;
+    for (int h = first; h < end; ++h) mine += units(length(h));
+    const int upto = wave_inclusive_scan_i32(mine);
+    if (lane == 63) s_sum[wave] = upto;
+    __syncthreads();
+    int before = upto - mine, total = 0;
+#pragma unroll
+    for (int v = 0; v < TC_WAVES; ++v) {
+        before += v < wave ? s_sum[v] : 0;
+        total += s_sum[v];
+    }
+    const int share = max((total + c.even - 1) / c.even, TREE_LEAST_UNITS), from = x * share;
+    if (x == 0) {   // for the merge
+        int at = before;
+        for (int h = first; h < end; ++h) {
+            c.units()[h] = at;
+            at += units(length(h));
+        }
+        if (tid == 0) {
+            c.units()[heads] = total;
+            c.units()[heads + 1] = share;
+        }
+    }
+    if (from >= total) return;
+    if (before <= from && from < before + mine) {
+        int h = first, at = before;
+        for (int u = units(length(h)); at + u <= from; u = units(length(h))) {
+            at += u;
+            ++h;
+        }
+        s_head = h;
+        s_unit = from - at;
+    }
+    __syncthreads();
+    int left = min(share, total - from), unit = s_unit;
+    for (int h = s_head; left > 0; ++h, unit = 0) {
+        const int n = length(h), take = min(left, units(n) - unit), lo = unit * TREE_UNIT;
+        if (take <= 0) continue;   // an empty cache
+        tree_cache_block<T, D, NQ, QG>(c, h, lo, min(n - lo, take * TREE_UNIT), h + x, lds);
+        left -= take;
+        __syncthreads();   // the LDS is free again
+    }
+}
+
+template <typename T, int D, int NT, int TURNS, bool EVEN>
 __global__ __launch_bounds__(TC_THREADS, 2) void tree_read_kernel(TreeCall c) {
     constexpr int PARTS = D / (64 * TURNS);   // blocks of a head's linear branch
     constexpr int NQ = NT == 1 ? 1 : 2, QG = NT <= 2 ? 1 : 2;
@@ -325,40 +381,57 @@ __global__ __launch_bounds__(TC_THREADS, 2) void tree_read_kernel(TreeCall c) {
     const int heads = c.B * c.H * c.G, id = blockIdx.x;
     if (id < heads * PARTS) {
         tree_linear_block<T, D, NT, TURNS>(c, id / PARTS, id % PARTS, s.linear);
+        return;
+    }
+    const int x = id - heads * PARTS;
+    auto length = [&](int h) { return min(max(c.cache_len[h], 0), c.cap); };
+    if constexpr (!EVEN) {
+        const int h = x / c.n_split, lo = x % c.n_split * c.rows, count = min(length(h) - lo, c.rows);
+        // (the merge knows from the same length which parts exist)
+        if (count > 0) tree_cache_block<T, D, NQ, QG>(c, h, lo, count, x, s.cache);
     } else {
-        const int x = id - heads * PARTS;
-        tree_cache_block<T, D, NQ, QG>(c, x / c.n_split, x % c.n_split, s.cache);
+        tree_even_block<T, D, NQ, QG>(c, x, heads, s.cache);
     }
 }
 
-template <typename T, int D, int TURNS>
+template <typename T, int D, int TURNS, bool EVEN>
 static void run_tree_read(const TreeCall& c, hipStream_t st) {
     const int heads = c.B * c.H * c.G;
-    const dim3 grid(heads * (D / (64 * TURNS)) + heads * c.n_split), block(TC_THREADS);
-    if (c.T <= 16) hipLaunchKernelGGL((tree_read_kernel<T, D, 1, TURNS>), grid, block, 0, st, c);
-    else if (c.T <= 32) hipLaunchKernelGGL((tree_read_kernel<T, D, 2, TURNS>), grid, block, 0, st, c);
-    else if (c.T <= 48) hipLaunchKernelGGL((tree_read_kernel<T, D, 3, TURNS>), grid, block, 0, st, c);
-    else hipLaunchKernelGGL((tree_read_kernel<T, D, 4, TURNS>), grid, block, 0, st, c);
+    const dim3 grid(heads * (D / (64 * TURNS)) + (EVEN ? c.even : heads * c.n_split)), block(TC_THREADS);
+    if (c.T <= 16) hipLaunchKernelGGL((tree_read_kernel<T, D, 1, TURNS, EVEN>), grid, block, 0, st, c);
+    else if (c.T <= 32) hipLaunchKernelGGL((tree_read_kernel<T, D, 2, TURNS, EVEN>), grid, block, 0, st, c);
+    else if (c.T <= 48) hipLaunchKernelGGL((tree_read_kernel<T, D, 3, TURNS, EVEN>), grid, block, 0, st, c);
+    else hipLaunchKernelGGL((tree_read_kernel<T, D, 4, TURNS, EVEN>), grid, block, 0, st, c);
 }
 
-// Rows of a part.  Large parts make few partial results (4 T d bytes each, written and read) and long runs of rows; small ones fill the chip
-// where there are few caches, and even out their lengths.  us of both kernels with parts of 256 / 512 / 1024 / 2048 rows: 1024 caches of
-// 64 .. 2048 rows, 16 nodes 207 / 187 / 176 / 171; 32 of 32000, 64 nodes 227 / 176 / 154 / 140; 96 of 64 .. 1024, 33 nodes 36 / 34 / 41 /
-// 41; 16 of 1000, 16 nodes 17 / 18 / 24 / 23 (128 rows: 19).
-int tree_cache_rows(const TreeCall& c) {
+// d = 128 with few heads: a head's linear branch in two blocks, which is the shorter chain
+static bool halves(const TreeCall& c) { return (long long)c.B * c.H * c.G <= 128; }
+
+// Parts of the caches.  Large parts make few partial results (4 T d bytes each, written and read) and long runs of rows; small ones fill the
+// chip where there are few caches.  us of both kernels with parts of 256 / 512 / 1024 / 2048 rows: 1024 caches of 64 .. 2048 rows, 16 nodes
+// 207 / 187 / 176 / 171; 32 of 32000, 64 nodes 227 / 176 / 154 / 140; 96 of 64 .. 1024, 33 nodes 36 / 34 / 41 / 41; 16 of 1000, 16 nodes 17 /
+// 18 / 24 / 23 (128 rows: 19).  With many caches the longest decide when parts are caches: then every block that fits the chip at once
+// takes the same number of rows (1024 caches of 64 .. 2048 rows 158 -> 149 us a call, 768 of 64 .. 2736 the read alone 168 -> 120, 768 of 1400 108 ->
+// 109).  That costs a scan of all lengths per block: nothing for fewer caches, nor for so many that their number evens out.
+void tree_cache_parts(TreeCall& c) {
     const long long heads = (long long)c.B * c.H * c.G;
-    int rows = 2048;
-    while (rows > 256 && heads * ((c.cap + rows - 1) / rows) < (rows > 512 ? 512 : 192)) rows /= 2;
-    return rows;
+    c.rows = 2048;
+    while (c.rows > 256 && heads * ((c.cap + c.rows - 1) / c.rows) < (c.rows > 512 ? 512 : 192)) c.rows /= 2;
+    c.n_split = (c.cap + c.rows - 1) / c.rows;
+    const int per_cu = c.d == 64 ? (c.T <= 48 ? 4 : 2) : (c.T <= 16 ? 3 : 2);   // blocks that a CU holds
+    c.even = !halves(c) && heads <= 2048 && heads * ((c.cap + 255) / 256) >= 1024 ? 256 * per_cu : 0;
 }
 
 nats_status launch_tree_read(const TreeCall& c, hipStream_t st) {
     ProfScope ps("tree_read", st);
-    // d = 128 with few heads: a head's linear branch in two blocks, which is the shorter chain
-    const bool halves = (long long)c.B * c.H * c.G <= 128;
-    if (c.d == 64) c.dtype == NATS_F32 ? run_tree_read<float, 64, 1>(c, st) : run_tree_read<bf16_t, 64, 1>(c, st);
-    else if (halves) c.dtype == NATS_F32 ? run_tree_read<float, 128, 1>(c, st) : run_tree_read<bf16_t, 128, 1>(c, st);
-    else c.dtype == NATS_F32 ? run_tree_read<float, 128, 2>(c, st) : run_tree_read<bf16_t, 128, 2>(c, st);
+    auto run = [&](auto zero) {
+        using T = decltype(zero);
+        if (c.d == 64) c.even ? run_tree_read<T, 64, 1, true>(c, st) : run_tree_read<T, 64, 1, false>(c, st);
+        else if (halves(c)) run_tree_read<T, 128, 1, false>(c, st);
+        else c.even ? run_tree_read<T, 128, 2, true>(c, st) : run_tree_read<T, 128, 2, false>(c, st);
+    };
+    if (c.dtype == NATS_F32) run(float{});
+    else run(bf16_t{});
     return check_launch("tree_read");
 }
 

@@ -316,3 +316,21 @@ def test_offsets_beyond_32_bits():
     y["cache_len"][0, H - 1] = cap
     y["v_cache"][0, H - 1, cap - 1] = math.inf
     assert torch.isinf(read(y)[0][0, H - 1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,T", [(64, 5), (128, 3), (64, 20), (128, 40), (64, 60)])
+def test_many_caches_in_equal_shares(dtype, d, T):
+    """More than 128 caches of very different lengths, empty ones among them: blocks that begin and end inside a cache and take several."""
+    B, H, cap = 11, 13, 1900
+    g = torch.Generator().manual_seed(d + T)
+    lens = (torch.rand(B, H, generator=g).pow(3) * (cap + 1)).int()
+    lens[2, 3:] = 0
+    lens[3, :9] = 0
+    lens[10, 12] = cap
+    x = ref.tree_inputs(B, H, T, d, cap, DT[dtype], seed=d + T, own_qk=True)
+    x["cache_len"] = lens
+    check(x)
+    x["cache_len"] = torch.zeros_like(lens)
+    x["cache_len"][5, 5] = 33
+    check(x)
