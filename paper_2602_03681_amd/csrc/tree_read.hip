@@ -371,7 +371,7 @@ __device__ __forceinline__ void tree_even_block(const TreeCall& c, int x, int he
 }
 
 template <typename T, int D, int NT, int TURNS, bool EVEN>
-__global__ __launch_bounds__(TC_THREADS, 2) void tree_read_kernel(TreeCall c) {
+__global__ __launch_bounds__(TC_THREADS, D == 64 ? 4 : 2) void tree_read_kernel(TreeCall c) {
     constexpr int PARTS = D / (64 * TURNS);   // blocks of a head's linear branch
     constexpr int NQ = NT == 1 ? 1 : 2, QG = NT <= 2 ? 1 : 2;
     __shared__ union {
@@ -411,15 +411,17 @@ static bool halves(const TreeCall& c) { return (long long)c.B * c.H * c.G <= 128
 // chip where there are few caches.  us of both kernels with parts of 256 / 512 / 1024 / 2048 rows: 1024 caches of 64 .. 2048 rows, 16 nodes
 // 207 / 187 / 176 / 171; 32 of 32000, 64 nodes 227 / 176 / 154 / 140; 96 of 64 .. 1024, 33 nodes 36 / 34 / 41 / 41; 16 of 1000, 16 nodes 17 /
 // 18 / 24 / 23 (128 rows: 19).  With many caches the longest decide when parts are caches: then every block that fits the chip at once
-// takes the same number of rows (1024 caches of 64 .. 2048 rows 158 -> 149 us a call, 768 of 64 .. 2736 the read alone 168 -> 120, 768 of 1400 108 ->
-// 109).  That costs a scan of all lengths per block: nothing for fewer caches, nor for so many that their number evens out.
+// takes the same number of rows (us a call, by caches and by shares: 1024 caches of 64 .. 2048 rows, 16 nodes 158 / 149; 512 of them, 33 nodes
+// 130 / 115; 384 in fp32, 20 nodes 175 / 131).  That costs a scan of all lengths per block and shares that end inside a cache: nothing for
+// fewer caches, for shorter ones (768 of 64 .. 1024, 64 nodes 148 / 159; 516 of 23 .. 418, d 64, 36 nodes 34 / 39), nor for so many that their
+// number evens out.
 void tree_cache_parts(TreeCall& c) {
     const long long heads = (long long)c.B * c.H * c.G;
     c.rows = 2048;
     while (c.rows > 256 && heads * ((c.cap + c.rows - 1) / c.rows) < (c.rows > 512 ? 512 : 192)) c.rows /= 2;
     c.n_split = (c.cap + c.rows - 1) / c.rows;
     const int per_cu = c.d == 64 ? (c.T <= 48 ? 4 : 2) : (c.T <= 16 ? 3 : 2);   // blocks that a CU holds
-    c.even = !halves(c) && heads <= 2048 && heads * ((c.cap + 255) / 256) >= 1024 ? 256 * per_cu : 0;
+    c.even = !halves(c) && c.cap > 1024 && heads <= 2048 ? 256 * per_cu : 0;
 }
 
 nats_status launch_tree_read(const TreeCall& c, hipStream_t st) {
