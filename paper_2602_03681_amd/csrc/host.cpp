@@ -412,7 +412,7 @@ PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t B = kc.size(0), H = kc.size(1), cap = kc.size(2), d = kc.size(3);
         const at::ScalarType dt = kc.scalar_type();
         nats_cache_evict_params p{(int)B, (int)H, (int)d, (int)cap, dtype_code(dt), integer(a[5]), integer(a[6])};
-        if (p.keep < 1) throw NotTaken();
+        if (p.keep < 1 || p.keep > cap) throw NotTaken();
         void* kp = here(kc, dt, {B, H, cap, d});
         void* vp = here(a[1], dt, {B, H, cap, d});
         void* len = here(a[2], at::kInt, {B, H});

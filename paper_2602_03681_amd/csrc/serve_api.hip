@@ -20,8 +20,8 @@ static nats_status check_pointers(std::initializer_list<const void*> needed, con
     return NATS_OK;
 }
 
-// sizes that all the operators share; heads: of the cache
-static nats_status check_cache(int dtype, int B, int H, int d, int cap, long long heads) {
+// sizes that all the operators share; the cache has H group heads
+static nats_status check_cache(int dtype, int B, int H, int d, int cap, int group) {
     if (dtype != NATS_F32 && dtype != NATS_BF16) {
         set_error("dtype %d is neither NATS_F32 nor NATS_BF16", dtype);
         return NATS_ERR_DTYPE;
@@ -31,7 +31,10 @@ static nats_status check_cache(int dtype, int B, int H, int d, int cap, long lon
         return NATS_ERR_SHAPE;
     }
     if (d != 64 && d != 128) { set_error("d must be 64 or 128 (got %d)", d); return NATS_ERR_SHAPE; }
-    if (heads > 65535) { set_error("the number of (batch, head) pairs must not exceed 65535 (got %lld)", heads); return NATS_ERR_SHAPE; }
+    if (B > 65535 || H > 65535 || (long long)B * H * group > 65535) {
+        set_error("the number of (batch, head) pairs must not exceed 65535 (got B %d, H %d, group %d)", B, H, group);
+        return NATS_ERR_SHAPE;
+    }
     if (cap > 1 << 20) { set_error("cap must not exceed 2^20 (got %d)", cap); return NATS_ERR_SHAPE; }
     return NATS_OK;
 }
@@ -39,7 +42,7 @@ static nats_status check_cache(int dtype, int B, int H, int d, int cap, long lon
 static nats_status check_tree_params(const nats_tree_params* p) {
     if (p == nullptr) { set_error("params is NULL"); return NATS_ERR_NULL; }
     if (p->group < 0 || p->group > 8) { set_error("group must be between 1 and 8 (0 counts as 1; got %d)", p->group); return NATS_ERR_SHAPE; }
-    const nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, (long long)p->B * p->H * (p->group ? p->group : 1));
+    const nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, p->group ? p->group : 1);
     if (st != NATS_OK) return st;
     if (p->T < 1 || p->T > NATS_TREE_MAX_NODES) {
         set_error("T must be between 1 and %d (got %d)", NATS_TREE_MAX_NODES, p->T);
@@ -64,7 +67,7 @@ static void set_tree_sizes(const nats_tree_params& p, TreeCall& c) {
 
 static nats_status check_weights_params(const nats_cache_weights_params* p) {
     if (p == nullptr) { set_error("params is NULL"); return NATS_ERR_NULL; }
-    const nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, (long long)p->B * p->H);
+    const nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, 1);
     if (st != NATS_OK) return st;
     if (p->T <= 0 || p->T > 1 << 20 || (long long)p->B * p->H * p->T > (1ll << 31) - 1) {
         set_error("T must be between 1 and 2^20 and B*H*T fit in 31 bits (T %d)", p->T);
@@ -114,6 +117,7 @@ nats_status nats_hybrid_attn_decode_tree(const nats_tree_params* p, const float*
     if (st != NATS_OK) return st;
     for (const void* in : {(const void*)state, k_cache, v_cache, q, k, v, p->q_nla, p->k_nla})
         if (o == in || (lse != nullptr && (const void*)lse == in)) { set_error("o and lse must not alias an input"); return NATS_ERR_SHAPE; }
+    if (o == (const void*)lse) { set_error("o and lse must be two arrays"); return NATS_ERR_SHAPE; }
     TreeCall c{};
     set_tree_sizes(*p, c);
     const size_t need = tree_workspace(c) * 4;
@@ -146,6 +150,12 @@ nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state
     }
     st = check_pointers({state, k_cache, v_cache, k, v}, "state, k_cache, v_cache, k and v", {p->k_nla});
     if (st != NATS_OK) return st;
+    if (k_cache == v_cache) { set_error("k_cache and v_cache must be two arrays"); return NATS_ERR_SHAPE; }
+    for (const void* in : {k, v, p->k_nla})
+        if ((const void*)state == in || k_cache == in || v_cache == in) {
+            set_error("state, k_cache and v_cache must not alias an input");
+            return NATS_ERR_SHAPE;
+        }
     TreeCommitCall c{};
     c.B = p->B; c.H = p->H; c.G = p->group ? p->group : 1; c.T = p->T; c.d = p->d; c.cap = p->cap; c.dtype = p->dtype;
     c.linear_op = p->linear_op; c.freeze = p->freeze_on_softmax;
@@ -190,7 +200,7 @@ nats_status nats_cache_weights(const nats_cache_weights_params* p, float* weight
 nats_status nats_cache_evict(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
                              int32_t* kept, void* hip_stream) {
     if (p == nullptr) { set_error("params is NULL"); return NATS_ERR_NULL; }
-    nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, (long long)p->B * p->H);
+    nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, 1);
     if (st != NATS_OK) return st;
     if (p->keep < 1 || p->keep > p->cap || p->recent < 0 || p->recent > p->keep) {
         set_error("keep must be between 1 and cap, recent between 0 and keep (cap %d, got %d, %d)", p->cap, p->keep, p->recent);

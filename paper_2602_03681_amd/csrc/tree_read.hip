@@ -361,7 +361,7 @@ __device__ __forceinline__ void tree_even_block(const TreeCall& c, int x, int he
     }
     __syncthreads();
     int left = min(share, total - from), unit = s_unit;
-    for (int h = s_head; left > 0; ++h, unit = 0) {
+    for (int h = s_head; left > 0 && h < heads; ++h, unit = 0) {
         const int n = length(h), take = min(left, units(n) - unit), lo = unit * TREE_UNIT;
         if (take <= 0) continue;   // an empty cache
         tree_cache_block<T, D, NQ, QG>(c, h, lo, min(n - lo, take * TREE_UNIT), h + x, lds);

@@ -225,8 +225,10 @@ def cache_evict(k_cache, v_cache, cache_len, weights, keep: int, recent: int = 0
     _require(v_cache, "v_cache", (B, H, cap, d), dt)
     _require(cache_len, "cache_len", (B, H), torch.int32)
     _require(weights, "weights", (B, H, cap), torch.float32)
-    kept = torch.empty((B, H, max(keep, 0)), dtype=torch.int32, device=k_cache.device) if kept is None else kept
-    _require(kept, "kept", (B, H, max(keep, 0)), torch.int32)
+    keep, recent = (max(-1, min(n, cap + 1)) for n in (keep, recent))   # (what is out of range is so in 32 bits, too)
+    rows = max(0, min(keep, cap))
+    kept = torch.empty((B, H, rows), dtype=torch.int32, device=k_cache.device) if kept is None else kept
+    _require(kept, "kept", (B, H, rows), torch.int32)
     _require_here(k_cache, v_cache, cache_len, weights, kept)
     p = CacheEvictParams(B, H, d, cap, _dtype_code(k_cache), keep, recent)
     _check(lib.nats_cache_evict(ctypes.byref(p), _ptr(k_cache), _ptr(v_cache), _ptr(cache_len), _ptr(weights), _ptr(kept),

@@ -77,8 +77,13 @@ def test_tree_pointers(lib):
         assert tree(lib, p, ptrs(16, p15=FAKE + 256 * i)) == E_SHAPE, i
     assert tree(lib, tree_params(q_nla=FAKE)) == E_NULL and tree(lib, tree_params(k_nla=FAKE)) == E_NULL
     assert tree(lib, tree_params(q_nla=FAKE, k_nla=FAKE + 8)) == E_ALIGN
+    assert tree(lib, p, ptrs(16, p15=FAKE + 256 * 14)) == E_SHAPE  # o and lse
     for i in range(11):                       # state .. node
         assert commit(lib, p, ptrs(13, **{f"p{i}": None})) == E_NULL, i
+    assert commit(lib, p, ptrs(13, p2=FAKE + 256)) == E_SHAPE      # k_cache and v_cache
+    for i in (0, 1, 2):
+        assert commit(lib, p, ptrs(13, p4=FAKE + 256 * i)) == E_SHAPE, i
+        assert commit(lib, p, ptrs(13, p5=FAKE + 256 * i)) == E_SHAPE, i
     for i in (0, 1, 2, 4, 5):
         assert commit(lib, p, ptrs(13, **{f"p{i}": FAKE + 8})) == E_ALIGN, i
     assert commit(lib, tree_params(k_nla=FAKE + 8)) == E_ALIGN
@@ -162,3 +167,9 @@ def test_tensors_that_are_not_on_the_gpu_or_of_another_shape(lib):
         nats.cache_weights(z(1, 2, 16), z(1, 2, 3, 64), st[1], st[3], vis=i(1, 4, 3))
     with pytest.raises(ValueError, match="GPU tensor"):
         nats.cache_evict(st[1], st[2], st[3], z(1, 2, 16), 8)
+
+
+def test_sizes_whose_product_passes_64_bits(lib):
+    big = dict(B=1 << 30, H=1 << 30)
+    assert tree(lib, tree_params(**big, group=8)) == E_SHAPE and commit(lib, tree_params(**big, group=8)) == E_SHAPE
+    assert evict(lib, B=(1 << 31) - 1, H=(1 << 31) - 1) == E_SHAPE
