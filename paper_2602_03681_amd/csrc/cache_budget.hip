@@ -22,6 +22,7 @@ constexpr float LOG2E = 1.44269504088896341f;
 constexpr int CW_THREADS = 256, CW_WAVES = CW_THREADS / 64;
 constexpr int CW_FEW = 64;       // queries that stay in registers
 constexpr int CW_KEEP = 16;      // queries whose logits are kept
+constexpr int CW_MOST_ROWS = 8192;   // of a part: a lane sums 512 of them one after the other
 
 // 16 rows of D elements as an operand (lane l16: row, lane quarter lq: its share of every 32 or 16 columns), and the product of two
 template <typename T, int D>
@@ -418,6 +419,12 @@ __global__ __launch_bounds__(CW_THREADS) void weights_join_kernel(WeightsCall c,
 size_t weights_workspace(WeightsCall& c, bool lse_given) {
     const long long heads = (long long)c.B * c.H;
     c.rows = heads * ((c.cap + 255) / 256) < 512 ? 128 : 256;
+    // Beyond 64 queries their groups of 64 are blocks, too, and load those queries, start a softmax and write a maximum and a sum per query
+    // for every part: larger parts, as long as eight blocks per CU are left (us of a call without lse, parts of 256 rows / these: 64 caches of
+    // 8192 rows, 8192 queries 4868 / 2882; 32 of 410, 8192 queries 234 / 140; 4 of 32768, 1024 queries 200 / 135, 156 with twice the
+    // blocks; 1024 of 2048, 128 queries 399 / 326; 140 of 2778 in fp32, 100 queries 275 / 263).
+    auto blocks_of_sums = [&] { return heads * ((c.cap + c.rows - 1) / c.rows) * ((c.T + 63) / 64); };
+    while (c.T > CW_FEW && c.rows < min(c.cap, CW_MOST_ROWS) && blocks_of_sums() > 2048) c.rows *= 2;
     c.parts = (c.cap + c.rows - 1) / c.rows;
     size_t at = 0;
     if (!lse_given) {

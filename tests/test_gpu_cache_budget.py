@@ -282,3 +282,60 @@ def test_more_queries_than_a_block_takes_at_once(T):
     _, lse = ref.cache_weights(**x, vis=vis)
     # the sums of T terms: by lanes, wavefronts and blocks, none of more than 1100 terms in a row
     check(x, vis=vis, lse=lse.float())
+
+
+def test_captured_weights_and_a_stream_of_the_callers_own():
+    """Few queries, more than keep their logits, and a prompt's; each with the sums taken here."""
+    cases = [inputs(2, 3, T, 64, 700, DT["bf16"], seed=91 + T) for T in (3, 40, 200)]
+    gs = [{k: v.cuda() for k, v in x.items()} for x in cases]
+    names = ("weights", "q", "k_cache", "cache_len")
+    first = [g["weights"].clone() for g in gs]
+    wants = []
+    for x in cases:
+        w = dict(x)
+        for _ in range(3):
+            w["weights"] = ref.cache_weights(**w, decay=0.5)[0]
+        wants.append(w["weights"])
+    eager = [[nats.cache_weights(*(g[n] for n in names), decay=0.5).clone() for _ in range(3)] for g in gs]
+    for x, e, want in zip(cases, eager, wants):
+        there = torch.arange(700) < x["cache_len"][..., None]
+        assert float(((e[2].cpu().double() - want).abs() / want.clamp_min(1e-30))[there].max()) <= 4 * TOL   # three calls, two of them decayed
+    for g, f in zip(gs, first):
+        g["weights"].copy_(f)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for g in gs:
+            nats.cache_weights(*(g[n] for n in names), decay=0.5)
+    for repeat in range(2):
+        for g, f in zip(gs, first):
+            g["weights"].copy_(f)
+        for step in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(g["weights"], e[step]) for g, e in zip(gs, eager))
+            torch.zeros(1 << 20, device="cuda").sum().item()
+    for g, f in zip(gs, first):
+        g["weights"].copy_(f)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for step in range(3):
+            for g, e in zip(gs, eager):
+                assert torch.equal(nats.cache_weights(*(g[n] for n in names), decay=0.5), e[step])
+
+
+def test_evict_sizes_that_do_not_fit_32_bits():
+    k, v, n, w = (t.cuda() for t in evict_inputs(1, 2, 64, 40, torch.bfloat16, seed=8, lens=40))
+    before = [t.clone() for t in (k, v, n, w)]
+    for keep, recent in (((1 << 32) + 5, 0), (41, 0), (0, 0), (-(1 << 32) + 5, 0), (5, 1 << 32), (5, -(1 << 32))):
+        with pytest.raises(nats.NatsError, match="keep must be"):
+            nats.cache_evict(k, v, n, w, keep, recent)
+    assert all(torch.equal(a, b) for a, b in zip(before, (k, v, n, w)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_parts_of_more_rows(dtype):
+    """More than 64 queries of many heads over long caches: parts of up to 8192 rows (512 terms of a lane's sum in a row: 3.1e-5 more)."""
+    x = inputs(1, 48, 100, 64, 9000, DT[dtype], seed=95)
+    check(x)
+    x = inputs(1, 3, 3000, 64, 9000, DT[dtype], seed=96)
+    check(x)
