@@ -334,3 +334,40 @@ def test_many_caches_in_equal_shares(dtype, d, T):
     x["cache_len"] = torch.zeros_like(lens)
     x["cache_len"][5, 5] = 33
     check(x)
+
+
+def test_captured_equal_shares_follow_the_lengths():
+    """One workspace, lengths that change between the replays: what the shares of one call left behind is of no use to the next."""
+    B, H, T, d, cap = 11, 13, 12, 128, 1900
+    x = cuda(ref.tree_inputs(B, H, T, d, cap, torch.bfloat16, seed=83))
+    g = torch.Generator().manual_seed(83)
+    lens = [torch.randint(0, cap + 1, (B, H), generator=g, dtype=torch.int32).cuda(),
+            torch.full((B, H), cap, dtype=torch.int32, device="cuda"), torch.zeros(B, H, dtype=torch.int32, device="cuda"),
+            (torch.arange(B * H, dtype=torch.int32, device="cuda") % 67).view(B, H)]
+    ws = torch.empty(nats.decode_tree_workspace_bytes(B, H, T, d, cap, nb.NATS_BF16), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(x["v"]), torch.empty(B, H, T, device="cuda")
+    wants = []
+    for n in lens:
+        x["cache_len"].copy_(n)
+        o, z = read(x)
+        wants.append((o.clone(), z.clone()))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        read(x, out=out, lse=lse, workspace=ws)
+    for repeat in range(2):
+        for n, (o, z) in zip(lens, wants):
+            x["cache_len"].copy_(n)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, o) and torch.equal(lse, z)
+            torch.zeros(1 << 20, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [16, 64])
+def test_keys_longer_than_one(dtype, T):
+    """Keys of length 2: a token's write overshoots, and the states grow along the path as they do token by token."""
+    x = ref.tree_inputs(1, 4, T, 128, 50, torch.float32, seed=89, p=0.0, tree="chain", lens=0)
+    x = {k: v.to(DT[dtype]) if k in ("k_cache", "v_cache", "q", "k", "v") else v for k, v in dict(x, k=2 * x["k"]).items()}
+    check(x)
