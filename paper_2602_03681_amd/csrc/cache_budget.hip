@@ -779,8 +779,9 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int ro
                                     (char*)(array == 0 ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + slice * SLICE, row_bytes);
 }
 
-// Both by one block per cache: where there are caches enough to fill the chip, one cache's selection hides behind another's rows (1024 caches
-// of 700 .. 2048 rows to 1024: 167 us + 13 us as two launches), and where there is little to move a launch is most of the time.
+// Both by one block per cache: with two caches per CU and more one's selection hides behind another's rows (us in one launch / in two: 2048
+// caches of 2000 .. 4096 rows to 1000, d 128 414 / 421; 1024 of 700 .. 2048 to 1024 185 / 184; 512 of 1000 .. 4096 to 2048, d 64 88 / 91;
+// but 256 of 700 .. 2048 to 1024 58 / 51: too few to hide anything), and where there is little to move a launch is most of the time.
 template <int THREADS, int PER, int ROW>
 __global__ __launch_bounds__(THREADS, 4) void evict_kernel(EvictCall c) {
     __shared__ SelectLds<THREADS> s;
@@ -795,7 +796,7 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(EvictCall c) {
 nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
     using std::integral_constant;
     const int heads = c.B * c.H, row_bytes = c.d * (c.dtype == NATS_F32 ? 4 : 2);
-    if (c.cap <= 4096 && (heads >= 256 || (long long)c.keep * row_bytes <= 128 << 10)) {
+    if (c.cap <= 4096 && (heads >= 512 || (long long)c.keep * row_bytes <= 128 << 10)) {
         ProfScope ps("evict", st);
         auto run = [&](auto per, auto row) {
             hipLaunchKernelGGL((evict_kernel<256, decltype(per)::value, decltype(row)::value>), dim3(heads), dim3(256), 0, st, c);
