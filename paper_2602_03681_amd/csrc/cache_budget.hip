@@ -530,27 +530,29 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One block per cache.  The weight of the last row that stays is found digit by digit: 8 bits of its key at a time, from counts of the
-// rows that agree in the digits so far.  The counts are kept in four copies, a lane's by its number: the first digit of attention weights
-// takes a dozen values, and lanes that add to one address go one after the other.  As soon as few enough rows agree, their keys go
-// into LDS and the other rows are left alone.  Then the rows above the weight found and the lowest of those equal to it are numbered in
-// order and their weights moved, behind them the last `recent` ones.  A wavefront has PER x 64 rows in a row, so that ranks inside it are
-// counts of ballot bits.  Up to THREADS x PER rows the keys stay in registers throughout; longer caches are gone through in such steps,
-// once per digit and once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its
-// old one).  With few caches it is bound by its instructions, on the few CUs that have one: about 30 per row and lane.
+// One block per cache.  The weight of the last row that stays is found by halving the range of keys 10 bits at a time: counts of the rows in
+// 1024 parts of the range that is left, which at first is that from the least key to the largest (with fixed digits most weights of an
+// attention share a dozen values of the first one, and lanes that add to one address go one after the other; for equal weights the counts are kept
+// in four copies, a lane's by its number).  As soon as a part stays as a whole its lower end is the border.  Then the rows above the
+// border, and the lowest of those equal to it, are numbered in order and their weights moved, behind them the last `recent` ones.  A wavefront
+// has up to PER x 64 rows in a row, as many as spread the cache over all wavefronts, so that ranks inside it are counts of ballot
+// bits.  Up to THREADS x PER rows the keys stay in registers throughout; longer caches are gone through in such steps, once per 10 bits and
+// once for the numbers (a step's rows are read before any of them is written, and no row's new place is behind its old one).  With few caches
+// it is bound by its instructions, on the few CUs that have one.
+constexpr int SELECT_BINS = 1024;
 template <int THREADS>
 struct SelectLds {
-    int4 hist[256];   // copy lane % 4 of every count
-    uint32_t few[8 * THREADS], digit;
-    int ties[THREADS / 64], stay[THREADS / 64], rest, agree, n;
+    int4 hist[SELECT_BINS];   // copy lane % 4 of every count
+    uint32_t least[THREADS / 64], most[THREADS / 64];
+    int sums[THREADS / 64], ties[THREADS / 64], stay[THREADS / 64], digit, rest, agree;
 };
 
 // false: the cache is within the budget, no row moves
 template <int THREADS, int PER>
 __device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectLds<THREADS>& s) {
-    constexpr int WAVES = THREADS / 64, STEP = THREADS * PER, FEW = 8 * THREADS;
+    constexpr int WAVES = THREADS / 64, GROUP = 2, BINS = SELECT_BINS / THREADS;   // GROUP: rows of a lane behind one branch
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = min(max(c.cache_len[bh], 0), c.cap);
+    const int n = __builtin_amdgcn_readfirstlane(min(max(c.cache_len[bh], 0), c.cap));
     float* w = c.weights + (size_t)bh * c.cap;
     int32_t* kept = c.kept + (size_t)bh * c.keep;
     if (n <= c.keep) {
@@ -559,153 +561,161 @@ __device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectL
     }
     const int m = n - c.recent;                       // the rows to choose from
     const int chosen = c.keep - c.recent;             // ... and how many of them stay
-    const bool one = m <= STEP;
+    const bool one = m <= THREADS * PER;
+    const int per = one ? (m + THREADS * GROUP - 1) / (THREADS * GROUP) * GROUP : PER, step = THREADS * per;   // rows of a lane and of the block
+    auto rows = [&](auto&& f) {   // f(i) for the lane's rows
+#pragma unroll
+        for (int g = 0; g < PER; g += GROUP)
+            if (g < per) {
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i) f(g + i);
+            }
+    };
+    float x[PER];
     uint32_t key[PER];
     auto load = [&](int r0) {
-        const int first = r0 + wave * 64 * PER;       // uniform
-        const float* x = w + first;
-        if (first + 64 * PER <= m) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = weight_key(x[(uint32_t)lane + 64u * i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int r = first + lane + 64 * i;
-                const uint32_t k = weight_key(w[(uint32_t)min(r, n - 1)]);
-                key[i] = r < m ? k : 0;
-            }
-        }
+        const int first = r0 + wave * 64 * per;       // uniform
+        rows([&](int i) { x[i] = w[(uint32_t)min(first + lane + 64 * i, n - 1)]; });
+        rows([&](int i) { key[i] = first + lane + 64 * i < m ? weight_key(x[i]) : 0; });
     };
-    if (one) load(0);
-    uint32_t prefix = 0;
-    int rest = chosen;   // of the rows that agree with `prefix`, this many stay
-    int few = -1;        // keys in LDS
     auto before = [&](uint64_t b) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, 0)); };
-    auto count = [&](uint32_t k, int shift) { atomicAdd(reinterpret_cast<int*>(&s.hist[(k >> shift) & 255]) + (lane & 3), 1); };
-    for (int shift = 24; chosen > 0 && shift >= 0; shift -= 8) {
-        const int above = shift + 8;
-        for (int i = tid; i < 256; i += THREADS) s.hist[i] = make_int4(0, 0, 0, 0);
-        __syncthreads();
-        if (few >= 0) {
-            for (int i = tid; i < few; i += THREADS)
-                if ((s.few[i] >> above) == (prefix >> above)) count(s.few[i], shift);
+    // the keys of the rows that may be the last to stay are base .. base + width, and `rest` of these stay (a key of 0 less base is above
+    // width: no key and no end of a range passes 32 bits)
+    uint32_t base = 1, width = 0xff800000u - 1;
+    int rest = chosen, agree = 0;
+    if (chosen > 0) {
+#pragma unroll
+        for (int i = 0; i < BINS; ++i) s.hist[tid * BINS + i] = make_int4(0, 0, 0, 0);
+        if (one) {
+            load(0);
+            uint32_t least = ~0u, most = 0;
+            rows([&](int i) {
+                least = min(least, key[i] - 1);       // (0 becomes the largest)
+                most = max(most, key[i]);
+            });
+            least = (uint32_t)wave_extreme_i32<false>((int)(least ^ 0x80000000u)) ^ 0x80000000u;
+            most = (uint32_t)wave_extreme_i32<true>((int)(most ^ 0x80000000u)) ^ 0x80000000u;
+            if (lane == 0) {
+                s.least[wave] = least;
+                s.most[wave] = most;
+            }
+            __syncthreads();
+            least = s.least[0];
+            most = s.most[0];
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) {
+                least = min(least, s.least[v]);
+                most = max(most, s.most[v]);
+            }
+            base = least + 1;
+            width = most - base;
         } else {
-            for (int r0 = 0; r0 < m; r0 += STEP) {
-                if (!one) load(r0);
-                if (shift == 24) {
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) count(key[i], 24);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < PER; ++i)
-                        if ((key[i] >> above) == (prefix >> above)) count(key[i], shift);
-                }
-            }
+            __syncthreads();
         }
-        __syncthreads();
-        if (wave == 0) {   // lane l: digits 255 - 4 l and the three below it
-            int h[4], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int4 x = s.hist[255 - 4 * lane - i];
-                sum += h[i] = x.x + x.y + x.z + x.w;
+        for (int shift = max(22 - __clz((int)width), 0);; shift = max(shift - 10, 0)) {   // width >> shift < 1024
+            for (int r0 = 0; r0 < m; r0 += step) {
+                if (!one) load(r0);
+                rows([&](int i) {
+                    const uint32_t k = key[i] - base;
+                    if (k <= width) atomicAdd(reinterpret_cast<int*>(&s.hist[k >> shift]) + (lane & 3), 1);
+                });
             }
-            int more = wave_inclusive_scan_i32(sum) - sum;
+            __syncthreads();
+            // a thread: BINS parts of the range, from the top
+            int h[BINS], sum = 0;
+#pragma unroll
+            for (int i = 0; i < BINS; ++i) {
+                int4& at = s.hist[SELECT_BINS - 1 - tid * BINS - i];
+                sum += h[i] = at.x + at.y + at.z + at.w;
+                at = make_int4(0, 0, 0, 0);
+            }
+            const int upto = wave_inclusive_scan_i32(sum);
+            if (lane == 63) s.sums[wave] = upto;
+            __syncthreads();
+            int more = upto - sum;
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) more += v < wave ? s.sums[v] : 0;
             if (more < rest && rest <= more + sum) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < BINS; ++i) {
                     if (more < rest && rest <= more + h[i]) {
-                        s.digit = 255 - 4 * lane - i;
+                        s.digit = SELECT_BINS - 1 - tid * BINS - i;
                         s.rest = rest - more;
                         s.agree = h[i];
                     }
                     more += h[i];
                 }
             }
-            if (lane == 0) s.n = 0;
-        }
-        __syncthreads();
-        prefix |= s.digit << shift;
-        rest = s.rest;
-        if (one && few < 0 && shift > 0 && s.agree <= FEW) {   // (in any order: they are only counted)
-            few = s.agree;
-            int mine = 0, at = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) mine += __popcll(__ballot((key[i] >> shift) == (prefix >> shift)));
-            if (lane == 0) at = atomicAdd(&s.n, mine);
-            at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const bool agrees = (key[i] >> shift) == (prefix >> shift);
-                const uint64_t b = __ballot(agrees);
-                if (agrees) s.few[at + before(b)] = key[i];
-                at += __popcll(b);
-            }
+            __syncthreads();
+            base += (uint32_t)s.digit << shift;
+            width = (1u << shift) - 1;
+            rest = s.rest;
+            agree = s.agree;
+            if (shift == 0 || agree == rest) break;
         }
     }
-    // (keys that stay are `prefix` at least, and more than 0: the rows that are not to be chosen do not reach it)
-    int done = 0, equal = 0;   // rows that stay, and rows equal to the last weight that stays, of the steps before
-    for (int r0 = 0; chosen > 0 && r0 < m; r0 += STEP) {
+    // rows with a key of `base` and more stay, and if these are too many, `rest` of those equal to it
+    int done = 0, equal = 0;   // rows that stay, and rows equal to `base`, of the steps before
+    for (int r0 = 0; chosen > 0 && r0 < m; r0 += step) {
         if (!one) load(r0);
-        int n_ties = 0, n_stay = 0;
+        if (agree > rest) {
+            int n_ties = 0;
+            rows([&](int i) { n_ties += __popcll(__ballot(key[i] == base)); });
+            if (lane == 0) s.ties[wave] = n_ties;
+            __syncthreads();
+            int rank = equal;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) n_ties += __popcll(__ballot(key[i] == prefix));
-        if (lane == 0) s.ties[wave] = n_ties;
-        __syncthreads();
-        int rank = equal;
-#pragma unroll
-        for (int v = 0; v < WAVES; ++v) {
-            if (v < wave) rank += s.ties[v];
-            equal += s.ties[v];
-        }
-        const float* mine = w + r0 + wave * 64 * PER;
-        uint32_t stays = 0;
-        float x[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            bool stay = key[i] > prefix;
-            const uint64_t b = __ballot(key[i] == prefix);
-            if (b != 0) {   // (uniform)
-                stay = stay || (key[i] == prefix && rank + before(b) < rest);
-                rank += __popcll(b);
+            for (int v = 0; v < WAVES; ++v) {
+                if (v < wave) rank += s.ties[v];
+                equal += s.ties[v];
             }
-            stays |= stay ? 1u << i : 0u;
-            n_stay += __popcll(__ballot(stay));
-            if (stay) x[i] = mine[(uint32_t)lane + 64u * i];
-            else x[i] = 0.f;
+            rows([&](int i) {
+                const uint64_t b = __ballot(key[i] == base);
+                if (b != 0) {   // (uniform)
+                    if (key[i] == base && rank + before(b) >= rest) key[i] = 0;
+                    rank += __popcll(b);
+                }
+            });
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(x[i]));   // every weight of the step has arrived before the barrier
+        int n_stay = 0;
+        rows([&](int i) { n_stay += __popcll(__ballot(key[i] >= base)); });
         if (lane == 0) s.stay[wave] = n_stay;
-        __syncthreads();
+        __syncthreads();   // the step's weights are in registers: a key was made of each
         int at = done;
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) {
             if (v < wave) at += s.stay[v];
             done += s.stay[v];
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const bool stay = (stays >> i) & 1;
+        const int mine = r0 + wave * 64 * per + lane;
+        rows([&](int i) {
+            const bool stay = key[i] >= base;
             const uint64_t b = __ballot(stay);
             if (stay) {
                 const uint32_t to = (uint32_t)(at + before(b));
                 w[to] = x[i];
-                kept[to] = r0 + wave * 64 * PER + lane + 64 * i;
+                kept[to] = mine + 64 * i;
             }
             at += __popcll(b);
-        }
+        });
+        if (!one) __syncthreads();   // s.ties and s.stay have been read
     }
     // the last rows, from m on to `chosen` on
-    for (int i0 = 0; i0 < c.recent; i0 += THREADS) {
-        const int i = i0 + tid;
-        float x = 0.f;
-        if (i < c.recent) x = w[m + i];
-        asm volatile("" : "+v"(x));
+    constexpr int TAIL = 4;   // per thread and step
+    for (int i0 = 0; i0 < c.recent; i0 += THREADS * TAIL) {
+        float y[TAIL];
+#pragma unroll
+        for (int j = 0; j < TAIL; ++j) y[j] = w[(uint32_t)min(m + i0 + j * THREADS + tid, n - 1)];
+#pragma unroll
+        for (int j = 0; j < TAIL; ++j) asm volatile("" : "+v"(y[j]));
         __syncthreads();   // (the chosen rows' weights were read before, and so were this step's)
-        if (i < c.recent) {
-            w[chosen + i] = x;
-            kept[chosen + i] = m + i;
+#pragma unroll
+        for (int j = 0; j < TAIL; ++j) {
+            const int i = i0 + j * THREADS + tid;
+            if (i < c.recent) {
+                w[chosen + i] = y[j];
+                kept[chosen + i] = m + i;
+            }
         }
     }
     if (tid == 0) c.cache_len[bh] = c.keep;
