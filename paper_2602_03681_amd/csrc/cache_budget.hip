@@ -784,7 +784,10 @@ __device__ __forceinline__ void evict_move_rows(const int32_t* kept, int keep, c
 
 template <int SLICE, int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictCall c, int row_bytes) {
-    const int bh = blockIdx.x, slices = row_bytes / SLICE, array = blockIdx.y / slices, slice = blockIdx.y % slices;
+    // blocks go to the eight XCDs in turn: the slices of an array to the same one, whose L2 then has the lines that they share
+    const int slices = row_bytes / SLICE, turn = blockIdx.x / 8, slice = turn % slices, of = turn / slices * 8 + blockIdx.x % 8;
+    const int bh = of / 2, array = of % 2;
+    if (bh >= c.B * c.H) return;
     evict_move_rows<SLICE, THREADS>(c.kept + (size_t)bh * c.keep, c.keep,
                                     (char*)(array == 0 ? c.k_cache : c.v_cache) + (size_t)bh * c.cap * row_bytes + slice * SLICE, row_bytes);
 }
@@ -830,7 +833,7 @@ nats_status launch_cache_evict(const EvictCall& c, hipStream_t st) {
     // 32000 rows to 8192: 35 us, 41 with 64 bytes, 47 with 256 threads)
     auto move = [&](auto slice, auto threads) {
         constexpr int SLICE = decltype(slice)::value, THREADS = decltype(threads)::value;
-        hipLaunchKernelGGL((evict_move_kernel<SLICE, THREADS>), dim3(heads, 2 * (row_bytes / SLICE)), dim3(THREADS), 0, st, c, row_bytes);
+        hipLaunchKernelGGL((evict_move_kernel<SLICE, THREADS>), dim3((2 * heads + 7) / 8 * 8 * (row_bytes / SLICE)), dim3(THREADS), 0, st, c, row_bytes);
     };
     const int bytes = heads * 2 * row_bytes;   // of a row of all caches, K and V
     if (row_bytes >= 256 && bytes >= 512 * 256) move(integral_constant<int, 256>{}, integral_constant<int, 256>{});
