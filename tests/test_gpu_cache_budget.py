@@ -339,3 +339,14 @@ def test_parts_of_more_rows(dtype):
     check(x)
     x = inputs(1, 3, 3000, 64, 9000, DT[dtype], seed=96)
     check(x)
+
+
+@pytest.mark.parametrize("cap,lens", [(1000, [[256, 511, 512, 513, 767]]), (4000, [[512, 513, 1023, 1025, 3585]]),
+                                      (9000, [[2047, 2048, 2049, 4097, 8193]]), (32800, [[32767, 32768, 32769, 2100, 30721]])])
+def test_evict_lengths_about_a_threads_rows(cap, lens):
+    """The rows of a cache are spread over the threads two by two each; the caches with and without a last share that is not whole."""
+    k, v, n, w = evict_inputs(1, 5, 64, cap, torch.bfloat16, seed=cap, lens=lens)
+    for keep, recent in ((200, 0), (200, 199), (200, 1), (255, 100)):
+        check_evict(k, v, n, w, keep, recent)
+    check_evict(k, v, n, torch.where(w < 0.5, w * 1e-30, (w * 4).floor()), 200, 7)     # a wide range of weights, many equal ones
+    check_evict(k, v, n, torch.full_like(w, 0.25), 200, 7)
