@@ -342,7 +342,7 @@ def test_parts_of_more_rows(dtype):
 
 
 @pytest.mark.parametrize("cap,lens", [(1000, [[256, 511, 512, 513, 767]]), (4000, [[512, 513, 1023, 1025, 3585]]),
-                                      (9000, [[2047, 2048, 2049, 4097, 8193]]), (32800, [[32767, 32768, 32769, 2100, 30721]])])
+                                      (9000, [[2047, 2048, 2049, 4097, 8193]]), (32800, [[32767, 32768, 32769, 2100, 28673]])])
 def test_evict_lengths_about_a_threads_rows(cap, lens):
     """The rows of a cache are spread over the threads two by two each; the caches with and without a last share that is not whole."""
     k, v, n, w = evict_inputs(1, 5, 64, cap, torch.bfloat16, seed=cap, lens=lens)
