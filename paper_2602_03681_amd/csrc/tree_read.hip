@@ -13,9 +13,10 @@
 //                                  tiles fill the 8 slots of a bf16 operand); A = V^T: a lane reads 8 (4) columns of the keys of
 //                                  its slots, and column 8 l + e of all lanes l is row l of tile e: the keys' halves of a column are
 //                                  joined by byte permutes (bf16) or stand as they came (fp32)
-// bf16 tensors: logits are exact products summed in fp32; P enters as the sum of two bf16 terms (17 bits), for one term (8 bits) would
-// show in fp32 outputs' accuracy and this kernel has matrix cycles to spare.  The upper term is cut off and the lower one kept above 0, so that
-// an infinity in V stays one.
+// bf16 tensors: logits are exact products summed in fp32; P enters as the sum of three bf16 terms, all of its 24 bits: with two (17 bits) ten
+// times as many outputs were rounded to the wrong neighbour, and this kernel has matrix cycles to spare (us of a call with two / three: 1024
+// caches of 64 .. 2048 rows, 16 nodes 148 / 148; 32 of 32000, 64 nodes 130 / 130; 96 of 64 .. 1024, 33 nodes 27.5 / 28.2).  Every term is cut
+// off, so that the last one is exact, and the lower two are kept above 0, so that an infinity in V stays one.
 #include <math.h>
 
 #include "mfma_util.h"
@@ -46,7 +47,7 @@ template <int D>
 struct CacheTile<bf16_t, D> {
     static constexpr int KT = 2, W = D / 32;   // W: 32-bit words of a V row per lane (D / 16 columns)
     using Query = u32x4[D / 32];               // column l16 of Q^T, elements 32 ks + 8 lq ..
-    using Weights = u32x4[2];                  // upper and lower terms
+    using Weights = u32x4[N_TERMS];            // the upper term first
     u32x4 k[KT][D / 32];
     uint32_t v[8][W];                          // slot s: key 16 (s / 4) + 4 lq + s % 4
     __device__ __forceinline__ static void load_query(const bf16_t* row, int lq, bool live, Query& q) {
@@ -96,10 +97,14 @@ struct CacheTile<bf16_t, D> {
     __device__ __forceinline__ static void weights(const f32x4 (&p)[KT], Weights& w) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
-            const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
-            w[0][i] = (hx >> 16) | hy;
-            w[1][i] = pack_bf16x2(fmaxf(x - __uint_as_float(hx), 0x1p-120f), fmaxf(y - __uint_as_float(hy), 0x1p-120f));
+            float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
+#pragma unroll
+            for (int n = 0; n < N_TERMS; ++n) {
+                const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
+                w[n][i] = (hx >> 16) | hy;
+                x = fmaxf(x - __uint_as_float(hx), 0x1p-120f);
+                y = fmaxf(y - __uint_as_float(hy), 0x1p-120f);
+            }
         }
     }
     // column `column(lq, j, e)` of the result is what element j of tile e holds
@@ -113,10 +118,9 @@ struct CacheTile<bf16_t, D> {
             for (int i = 0; i < 4; ++i)
                 a[i] = __builtin_amdgcn_perm(v[2 * i + 1][e / 2], v[2 * i][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                o[n][e] = mfma_bf16(a, w[n][0], o[n][e]);
-                o[n][e] = mfma_bf16(a, w[n][1], o[n][e]);
-            }
+            for (int i = N_TERMS - 1; i >= 0; --i)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[n][e] = mfma_bf16(a, w[n][i], o[n][e]);
         }
     }
 };
