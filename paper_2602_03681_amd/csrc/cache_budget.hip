@@ -207,11 +207,17 @@ __global__ __launch_bounds__(CW_THREADS) void weights_kept_kernel(WeightsCall c)
     join(m, l, lane_xor16(m, lane), lane_xor16(l, lane));
     join(m, l, lane_xor32(m, lane), lane_xor32(l, lane));
     const float lse = l == 0.f ? INFINITY : m + log2f(l);   // (a query that sees nothing: all its logits are -inf)
+    const int vis = sees_rows(c, bh, t, n);
 #pragma unroll 4
     for (int q = 0; q < c.T; ++q) {
         const float L = __shfl(lse, q);
+        const int seen = __shfl(vis, q);
 #pragma unroll
-        for (int i = 0; i < CW_KEPT_ROWS; ++i) sum[i] += __builtin_amdgcn_exp2f(z[(size_t)q * c.pitch + min(r0 + i * CW_THREADS, n - 1)] - L);
+        for (int i = 0; i < CW_KEPT_ROWS; ++i) {
+            const int r = min(r0 + i * CW_THREADS, n - 1);
+            const float p = __builtin_amdgcn_exp2f(z[(size_t)q * c.pitch + r] - L);
+            sum[i] += r < seen ? p : 0.f;   // (L may be NaN: in a row that the query does not see, p is then one, too)
+        }
     }
 #pragma unroll
     for (int i = 0; i < CW_KEPT_ROWS; ++i)
