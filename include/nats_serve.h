@@ -10,7 +10,9 @@
  *   (the caller accepts a path of the tree)
  *   nats_hybrid_attn_tree_commit   writes the accepted path into the state, its softmax tokens into the cache
  *   nats_cache_weights             adds the attention weight that the path's queries gave to every row of the cache
- *   nats_cache_evict               cuts the cache down to a budget by those weights
+ *   nats_cache_evict_clear         cuts the cache down to a budget by those weights
+ * The weights of rows that are not there have to be 0, for nats_cache_weights adds to what it finds and neither the commit nor the
+ * decode steps touch them: an array of zeros at first, and nats_cache_evict_clear keeps it so.
  */
 #ifndef NATS_SERVE_H_
 #define NATS_SERVE_H_
@@ -86,7 +88,7 @@ typedef struct nats_cache_weights_params {
 } nats_cache_weights_params;
 
 /* weights[c] <- decay * weights[c] + sum over the queries t that see row c (c < vis_t) of exp(scale * q_t . k_cache[c] - lse_t), for the
- * rows c < cache_len; the others are left as they are.
+ * rows c < cache_len; the others are left as they are (0 for a row that is to be appended, see above).
  *   weights : in/out [B,H,cap] f32;  q : in, dtype;  k_cache : in [B,H,cap,d];  cache_len : in [B,H] i32
  *   vis     : in i32 or NULL (every query sees every row): rows of the cache that query t sees, counted from row 0 (the forward's cnt,
  *             the commit's vis); more than cache_len counts as cache_len
@@ -108,9 +110,14 @@ typedef struct nats_cache_evict_params {
  * (of equal weights the lower row; a NaN counts as the lowest weight, -0 as 0), in their order: k_cache, v_cache and weights are
  * compacted in place, rows behind the first `keep` are left as they are, cache_len becomes `keep`.  Shorter caches stay as they are.
  * (Routing per chunk: between a commit and the next token, when no rows are provisional.)
- *   kept : out [B,H,keep] i32: the row that row r was before; -1 for rows that are not there */
+ *   kept : out [B,H,keep] i32: the row that row r was before; -1 for rows that are not there
+ * nats_cache_evict leaves the weights behind the first `keep` rows as they are, too: rows that are appended there later start with
+ * them, unless the caller clears them (a caller that keeps the weights of the rows before, or that starts them anew, has no need to). */
 nats_status nats_cache_evict(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
                              int32_t* kept, void* hip_stream);
+/* The same, and the weights of the rows that a cache gives up, `keep` .. cache_len - 1, become 0: what is appended starts with nothing. */
+nats_status nats_cache_evict_clear(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
+                                   int32_t* kept, void* hip_stream);
 
 #ifdef __cplusplus
 }

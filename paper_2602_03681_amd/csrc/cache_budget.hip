@@ -724,6 +724,10 @@ __device__ __forceinline__ bool evict_select(const EvictCall& c, int bh, SelectL
             }
         }
     }
+    if (c.clear) {
+        __syncthreads();   // the last rows' weights have been read
+        for (int r = c.keep + tid; r < n; r += THREADS) w[r] = 0.f;
+    }
     if (tid == 0) c.cache_len[bh] = c.keep;
     return true;
 }

@@ -402,10 +402,10 @@ PyObject* cache_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent) -> kept
+// cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent, clear_weights) -> kept
 PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        if (n != 7) throw NotTaken();
+        if (n != 8) throw NotTaken();
         Here here;
         const at::Tensor& kc = tensor(a[0]);
         if (kc.dim() != 4) throw NotTaken();
@@ -419,10 +419,9 @@ PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* wp = here(a[3], at::kFloat, {B, H, cap});
         const at::Tensor kept = given_or_new(a[4], {B, H, (int64_t)p.keep}, kc, at::kInt);
         void* keptp = here(kept, at::kInt, {B, H, (int64_t)p.keep});
+        const auto evict = integer(a[7]) ? nats_cache_evict_clear : nats_cache_evict;
         void* const stream = current_stream();
-        return status(unlocked([&] {
-            return nats_cache_evict(&p, kp, vp, (int32_t*)len, (float*)wp, (int32_t*)keptp, stream);
-        }), kept);
+        return status(unlocked([&] { return evict(&p, kp, vp, (int32_t*)len, (float*)wp, (int32_t*)keptp, stream); }), kept);
     });
 }
 

@@ -75,6 +75,7 @@ struct EvictCall {
     int32_t* cache_len;
     float* weights;
     int32_t* kept;
+    int clear;             // the weights behind the rows that stay become 0
 };
 nats_status launch_cache_evict(const EvictCall& c, hipStream_t st);
 

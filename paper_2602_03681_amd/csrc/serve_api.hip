@@ -197,8 +197,8 @@ nats_status nats_cache_weights(const nats_cache_weights_params* p, float* weight
     return launch_cache_weights(c, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
-nats_status nats_cache_evict(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
-                             int32_t* kept, void* hip_stream) {
+static nats_status evict(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
+                         int32_t* kept, int clear, void* hip_stream) {
     if (p == nullptr) { set_error("params is NULL"); return NATS_ERR_NULL; }
     nats_status st = check_cache(p->dtype, p->B, p->H, p->d, p->cap, 1);
     if (st != NATS_OK) return st;
@@ -210,8 +210,18 @@ nats_status nats_cache_evict(const nats_cache_evict_params* p, void* k_cache, vo
     st = check_pointers({k_cache, v_cache, weights}, "k_cache, v_cache and weights", {});
     if (st != NATS_OK) return st;
     if (k_cache == v_cache) { set_error("k_cache and v_cache must be two arrays"); return NATS_ERR_SHAPE; }
-    EvictCall c{p->B, p->H, p->d, p->cap, p->dtype, p->keep, p->recent, k_cache, v_cache, cache_len, weights, kept};
+    EvictCall c{p->B, p->H, p->d, p->cap, p->dtype, p->keep, p->recent, k_cache, v_cache, cache_len, weights, kept, clear};
     return launch_cache_evict(c, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+nats_status nats_cache_evict(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
+                             int32_t* kept, void* hip_stream) {
+    return evict(p, k_cache, v_cache, cache_len, weights, kept, 0, hip_stream);
+}
+
+nats_status nats_cache_evict_clear(const nats_cache_evict_params* p, void* k_cache, void* v_cache, int32_t* cache_len, float* weights,
+                                   int32_t* kept, void* hip_stream) {
+    return evict(p, k_cache, v_cache, cache_len, weights, kept, 1, hip_stream);
 }
 
 }  // extern "C"

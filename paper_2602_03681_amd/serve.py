@@ -48,8 +48,9 @@ def declare(lib) -> None:
     lib.nats_cache_weights_workspace_bytes.argtypes = [ctypes.POINTER(CacheWeightsParams), ctypes.c_int32]
     lib.nats_cache_weights.restype = ctypes.c_int
     lib.nats_cache_weights.argtypes = [ctypes.POINTER(CacheWeightsParams)] + [vp] * 7 + [size, vp]
-    lib.nats_cache_evict.restype = ctypes.c_int
-    lib.nats_cache_evict.argtypes = [ctypes.POINTER(CacheEvictParams)] + [vp] * 6
+    for evict in (lib.nats_cache_evict, lib.nats_cache_evict_clear):
+        evict.restype = ctypes.c_int
+        evict.argtypes = [ctypes.POINTER(CacheEvictParams)] + [vp] * 6
 
 
 def _require_here(*tensors: Optional[torch.Tensor]) -> None:
@@ -178,7 +179,8 @@ def cache_weights(weights, q, k_cache, cache_len, *, lse=None, vis=None, softmax
                   workspace=None) -> torch.Tensor:
     """nats_cache_weights: weights [B,H,cap] f32 <- decay * weights + the attention weight that the queries q [B,Hq,T,d] give to the
     rows of the cache, in place.  Hq divides H (a query head serves H / Hq heads of the cache in a row), so does the number of heads
-    of vis [B,Hv,T] i32 (rows that a query sees; None: all).  lse [B,H,T] f32: None: taken over the rows that a query sees."""
+    of vis [B,Hv,T] i32 (rows that a query sees; None: all).  lse [B,H,T] f32: None: taken over the rows that a query sees.
+    A row that is appended later starts with what stands in weights at its place: 0, in an array of zeros that evictions clear."""
     lib = nb.load_library()
     r = nb._host.cache_weights(weights, q, k_cache, cache_len, lse, vis, workspace, softmax_scale, decay)
     if r is not None:
@@ -210,11 +212,15 @@ def cache_weights(weights, q, k_cache, cache_len, *, lse=None, vis=None, softmax
     return weights
 
 
-def cache_evict(k_cache, v_cache, cache_len, weights, keep: int, recent: int = 0, *, kept=None) -> torch.Tensor:
+def cache_evict(k_cache, v_cache, cache_len, weights, keep: int, recent: int = 0, *, kept=None,
+                clear_weights: bool = False) -> torch.Tensor:
     """nats_cache_evict: caches of more than `keep` rows keep their last `recent` rows and the heaviest of the others, in order and in
-    place (k_cache, v_cache, weights, cache_len) -> kept [B,H,keep] i32, the row that each row was before (-1: no row)."""
+    place (k_cache, v_cache, weights, cache_len) -> kept [B,H,keep] i32, the row that each row was before (-1: no row).
+
+    clear_weights: the weights of the rows that are given up become 0 (nats_cache_evict_clear).  Wanted wherever weights go on being
+    added up while rows are appended; without it a new row starts with the weight of the one that lay in its place."""
     lib = nb.load_library()
-    r = nb._host.cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent)
+    r = nb._host.cache_evict(k_cache, v_cache, cache_len, weights, kept, keep, recent, clear_weights)
     if r is not None:
         if type(r) is int:
             _check(r)
@@ -231,6 +237,6 @@ def cache_evict(k_cache, v_cache, cache_len, weights, keep: int, recent: int = 0
     _require(kept, "kept", (B, H, rows), torch.int32)
     _require_here(k_cache, v_cache, cache_len, weights, kept)
     p = CacheEvictParams(B, H, d, cap, _dtype_code(k_cache), keep, recent)
-    _check(lib.nats_cache_evict(ctypes.byref(p), _ptr(k_cache), _ptr(v_cache), _ptr(cache_len), _ptr(weights), _ptr(kept),
-                                _stream_ptr()))
+    evict = lib.nats_cache_evict_clear if clear_weights else lib.nats_cache_evict
+    _check(evict(ctypes.byref(p), _ptr(k_cache), _ptr(v_cache), _ptr(cache_len), _ptr(weights), _ptr(kept), _stream_ptr()))
     return kept
