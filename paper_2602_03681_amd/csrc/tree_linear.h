@@ -143,6 +143,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         const int ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
         const int j = 16 * tj + l16;
         const double lgj = s.lg[j];
+        const bool writes = s.b[j] != 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = 16 * ti + 4 * lq + e;
@@ -154,8 +155,9 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 r = 1.f;
                 for (int m = i; m != j; m = s.par[m]) r *= s.a[m];
             }
-            s.n[i][j] = on && i != j ? -s.b[i] * r * kk[x][e] : 0.f;
-            s.p[i][j] = on ? r * qk[x][e] : 0.f;
+            // (a node that writes nothing: its key may hold anything)
+            s.n[i][j] = on && i != j && writes ? -s.b[i] * r * kk[x][e] : 0.f;
+            s.p[i][j] = on && writes ? r * qk[x][e] : 0.f;
         }
     }
     __syncthreads();
