@@ -160,7 +160,8 @@ __global__ __launch_bounds__(MERGE_THREADS) void tree_merge_kernel(TreeCall c) {
 // A block per output head.  Eight lanes hold a row of S (D / 8 elements each), and the rows are independent of one another, so that the path's
 // tokens follow each other without a barrier; eight tokens at a time come through LDS.  The state is kept as S / G with G the product
 // of the decays so far: a softmax token then costs nothing and a linear one two operations per element, the product with k and
-// the update (S would take a third).  G is taken back into S where it leaves 2^-40 .. 2^40.
+// the update (S would take a third).  G is taken back into S where it leaves 2^-40 .. 2.  S / G leaves fp32's range before S does, by as
+// much as 2^40; a wavefront whose rows are not all finite at the end takes its tokens again, S by S.
 constexpr int COMMIT_THREADS = 256, COMMIT_TOKENS = 8;
 
 template <typename T, int D>
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
         for (int i = 0; i < here; ++i) {
             const float bt = s_b[first + i];
             G *= s_a[first + i];
-            if (!(fabsf(G) > 0x1p-40f && fabsf(G) < 0x1p40f)) {
+            if (!(fabsf(G) > 0x1p-40f && fabsf(G) < 2.f)) {
 #pragma unroll
                 for (int p = 0; p < PASSES; ++p)
 #pragma unroll
@@ -250,6 +251,46 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
                     u -= G * lane_group_sum<LPR>(pred);
                 }
                 u *= bt * inv;
+#pragma unroll
+                for (int x = 0; x < W; ++x) S[p][x] += u * kk[x];
+            }
+        }
+    }
+    bool fine = true;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+        for (int x = 0; x < W; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) fine = fine && fabsf(S[p][x][e]) < INFINITY;
+    if (!__all(fine)) {
+        G = 1.f;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+            for (int x = 0; x < W; ++x) S[p][x] = *reinterpret_cast<const f32x4*>(Sb + (size_t)(p * PER_PASS + r0) * D + 32 * x + 4 * lr);
+        for (int i = 0; i < n; ++i) {
+            const int t = s_path[i];
+            const float a = s_a[i], bt = s_b[i];
+            f32x4 kk[W];
+#pragma unroll
+            for (int x = 0; x < W; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kk[x][e] = to_float(k[t * D + 32 * x + 4 * lr + e]);
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+#pragma unroll
+                for (int x = 0; x < W; ++x) S[p][x] *= a;
+                if (bt == 0.f) continue;
+                float u = to_float(v[t * D + p * PER_PASS + r0]);
+                if (c.linear_op == 0) {
+                    float pred = 0.f;
+#pragma unroll
+                    for (int x = 0; x < W; ++x)
+                        pred += S[p][x][0] * kk[x][0] + S[p][x][1] * kk[x][1] + S[p][x][2] * kk[x][2] + S[p][x][3] * kk[x][3];
+                    u -= lane_group_sum<LPR>(pred);
+                }
+                u *= bt;
 #pragma unroll
                 for (int x = 0; x < W; ++x) S[p][x] += u * kk[x];
             }
