@@ -8,7 +8,7 @@
  * A round of generation from drafts:
  *   nats_hybrid_attn_decode_tree   reads a tree of drafted tokens against the state and the cache; changes neither
  *   (the caller accepts a path of the tree)
- *   nats_hybrid_attn_tree_commit   writes the accepted path into the state, its softmax tokens into the cache
+ *   nats_hybrid_attn_tree_commit   writes the accepted path into the state, its softmax tokens into the cache (padded trees: .._ex)
  *   nats_cache_weights             adds the attention weight that the path's queries gave to every row of the cache
  *   nats_cache_evict_clear         cuts the cache down to a budget by those weights
  * The weights of rows that are not there have to be 0, for nats_cache_weights adds to what it finds and neither the commit nor the
@@ -70,12 +70,18 @@ nats_status nats_hybrid_attn_decode_tree(const nats_tree_params* p, const float*
  *   vis       : out [B,H*G,T] i32 or NULL: for a node of the path the rows of the cache, as it is now, that the node saw: those that
  *               were there and the path's softmax tokens up to the node itself; 0 for the other nodes
  *   err_flags : out [B,H*G] i32 or NULL: 1 where a softmax token found the cache full (it is not stored, and no later one is),
- *               2 where node[b] is no node (nothing is done then), else 0
+ *               2 where node[b] is no node, that is none of -1 .. T - 1 (nothing is done then), else 0
  * p->softmax_scale, la_scale, combine_mode, rms_eps and q_nla are not read. */
 nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state, void* k_cache, void* v_cache, int32_t* cache_len,
                                          const void* k, const void* v, const float* alpha, const float* beta, const uint8_t* mask,
                                          const int32_t* parent, const int32_t* node, int32_t* vis, int32_t* err_flags,
                                          void* hip_stream);
+/* The same for padded trees: nodes i >= n_nodes[b] are not there (as in the call that read the tree; [B] i32 or NULL: T), and a node[b]
+ * that is not there is no node: flag 2, nothing is done. */
+nats_status nats_hybrid_attn_tree_commit_ex(const nats_tree_params* p, float* state, void* k_cache, void* v_cache, int32_t* cache_len,
+                                            const void* k, const void* v, const float* alpha, const float* beta, const uint8_t* mask,
+                                            const int32_t* parent, const int32_t* n_nodes, const int32_t* node, int32_t* vis,
+                                            int32_t* err_flags, void* hip_stream);
 
 typedef struct nats_cache_weights_params {
     int32_t B, H;          /* sequences, heads of the cache (all output heads)                         */

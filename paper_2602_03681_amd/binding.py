@@ -78,7 +78,7 @@ EXPORTS = ("nats_hybrid_attn_fwd_workspace_bytes", "nats_hybrid_attn_fwd", "nats
            "nats_hybrid_attn_bwd_workspace_bytes", "nats_hybrid_attn_bwd", "nats_hybrid_attn_bwd_bf16",
            "nats_hybrid_attn_fwd_noalloc",
            "nats_hybrid_attn_decode_workspace_bytes", "nats_merge_weights_from_x",
-           "nats_hybrid_attn_decode_tree_workspace_bytes", "nats_hybrid_attn_decode_tree", "nats_hybrid_attn_tree_commit",
+           "nats_hybrid_attn_decode_tree_workspace_bytes", "nats_hybrid_attn_decode_tree", "nats_hybrid_attn_tree_commit", "nats_hybrid_attn_tree_commit_ex",
            "nats_cache_weights_workspace_bytes", "nats_cache_weights", "nats_cache_evict", "nats_cache_evict_clear")
 
 

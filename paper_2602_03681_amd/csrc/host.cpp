@@ -327,15 +327,15 @@ PyObject* decode_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, k_nla, vis, err_flags, linear_op,
+// tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, n_nodes, k_nla, vis, err_flags, linear_op,
 //             freeze_on_softmax, group) -> vis
 PyObject* tree_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        if (n != 17) throw NotTaken();
+        if (n != 18) throw NotTaken();
         Here here;
         const at::Tensor &kc = tensor(a[1]), &k = tensor(a[4]), &v = tensor(a[5]);
         nats_tree_params p{};
-        tree_sizes(p, k, kc, integer(a[16]));
+        tree_sizes(p, k, kc, integer(a[17]));
         const int64_t B = p.B, H = p.H, T = p.T, d = p.d, cap = p.cap, HG = kc.size(1);
         const at::ScalarType dt = kc.scalar_type();
         void* state = here(a[0], at::kFloat, {B, HG, d, d});
@@ -349,17 +349,18 @@ PyObject* tree_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* mask = here(a[8], at::kByte, {B, H, T});
         void* parent = here(a[9], at::kInt, {B, T});
         void* node = here(a[10], at::kInt, {B});
-        p.k_nla = here.optional(a[11], dt, {B, HG, T, d});
-        void* err = here.optional(a[13], at::kInt, {B, HG});
-        p.linear_op = integer(a[14]);
-        p.freeze_on_softmax = integer(a[15]);
-        const at::Tensor vis = given_or_new(a[12], {B, HG, T}, v, at::kInt);
+        void* nodes = here.optional(a[11], at::kInt, {B});
+        p.k_nla = here.optional(a[12], dt, {B, HG, T, d});
+        void* err = here.optional(a[14], at::kInt, {B, HG});
+        p.linear_op = integer(a[15]);
+        p.freeze_on_softmax = integer(a[16]);
+        const at::Tensor vis = given_or_new(a[13], {B, HG, T}, v, at::kInt);
         void* visp = here(vis, at::kInt, {B, HG, T});
         void* const stream = current_stream();
         return status(unlocked([&] {
-            return nats_hybrid_attn_tree_commit(&p, (float*)state, kcache, vcache, (int32_t*)len, kp, vp, (const float*)alpha,
-                                                (const float*)beta, (const uint8_t*)mask, (const int32_t*)parent, (const int32_t*)node,
-                                                (int32_t*)visp, (int32_t*)err, stream);
+            return nats_hybrid_attn_tree_commit_ex(&p, (float*)state, kcache, vcache, (int32_t*)len, kp, vp, (const float*)alpha,
+                                                   (const float*)beta, (const uint8_t*)mask, (const int32_t*)parent,
+                                                   (const int32_t*)nodes, (const int32_t*)node, (int32_t*)visp, (int32_t*)err, stream);
         }), vis);
     });
 }

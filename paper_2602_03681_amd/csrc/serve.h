@@ -46,7 +46,7 @@ struct TreeCommitCall {
     const void *k, *v, *k_nla;
     const float *alpha, *beta;
     const uint8_t* mask;
-    const int32_t *parent, *node;
+    const int32_t *parent, *n_nodes, *node;
     int32_t *vis, *err_flags;
 };
 nats_status launch_tree_commit(const TreeCommitCall& c, hipStream_t st);

@@ -138,10 +138,10 @@ nats_status nats_hybrid_attn_decode_tree(const nats_tree_params* p, const float*
     return launch_tree(c, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
-nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state, void* k_cache, void* v_cache, int32_t* cache_len,
-                                         const void* k, const void* v, const float* alpha, const float* beta, const uint8_t* mask,
-                                         const int32_t* parent, const int32_t* node, int32_t* vis, int32_t* err_flags,
-                                         void* hip_stream) {
+nats_status nats_hybrid_attn_tree_commit_ex(const nats_tree_params* p, float* state, void* k_cache, void* v_cache, int32_t* cache_len,
+                                            const void* k, const void* v, const float* alpha, const float* beta, const uint8_t* mask,
+                                            const int32_t* parent, const int32_t* n_nodes, const int32_t* node, int32_t* vis,
+                                            int32_t* err_flags, void* hip_stream) {
     nats_status st = check_tree_params(p);
     if (st != NATS_OK) return st;
     if (!cache_len || !alpha || !beta || !mask || !parent || !node) {
@@ -160,9 +160,17 @@ nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state
     c.B = p->B; c.H = p->H; c.G = p->group ? p->group : 1; c.T = p->T; c.d = p->d; c.cap = p->cap; c.dtype = p->dtype;
     c.linear_op = p->linear_op; c.freeze = p->freeze_on_softmax;
     c.state = state; c.k_cache = k_cache; c.v_cache = v_cache; c.cache_len = cache_len;
-    c.k = k; c.v = v; c.k_nla = p->k_nla; c.alpha = alpha; c.beta = beta; c.mask = mask; c.parent = parent; c.node = node;
-    c.vis = vis; c.err_flags = err_flags;
+    c.k = k; c.v = v; c.k_nla = p->k_nla; c.alpha = alpha; c.beta = beta; c.mask = mask; c.parent = parent;
+    c.n_nodes = n_nodes; c.node = node; c.vis = vis; c.err_flags = err_flags;
     return launch_tree_commit(c, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+nats_status nats_hybrid_attn_tree_commit(const nats_tree_params* p, float* state, void* k_cache, void* v_cache, int32_t* cache_len,
+                                         const void* k, const void* v, const float* alpha, const float* beta, const uint8_t* mask,
+                                         const int32_t* parent, const int32_t* node, int32_t* vis, int32_t* err_flags,
+                                         void* hip_stream) {
+    return nats_hybrid_attn_tree_commit_ex(p, state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, nullptr, node, vis,
+                                           err_flags, hip_stream);
 }
 
 size_t nats_cache_weights_workspace_bytes(const nats_cache_weights_params* p, int32_t lse_given) {

@@ -180,8 +180,8 @@ __global__ __launch_bounds__(COMMIT_THREADS) void tree_commit_kernel(TreeCommitC
 #pragma unroll
         for (int x = 0; x < W; ++x) S[p][x] = *reinterpret_cast<const f32x4*>(Sb + (size_t)(p * PER_PASS + r0) * D + 32 * x + 4 * lr);
     if (tid < 64) {
-        const int node = c.node[b];
-        const bool refused = node < -1 || node >= N, none = refused || node < 0;
+        const int node = c.node[b], there = c.n_nodes != nullptr ? min(max(c.n_nodes[b], 0), N) : N;
+        const bool refused = node < -1 || node >= there, none = refused || node < 0;
         const bool softmax = c.mask[(size_t)bh * N + min(tid, N - 1)] != 0;
         const float alpha = c.alpha[(size_t)bh * N + min(tid, N - 1)], beta = c.beta[(size_t)bh * N + min(tid, N - 1)];
         const int len = c.cache_len[bhg], had = min(max(len, 0), c.cap), room = len < 0 ? 0 : c.cap - had;

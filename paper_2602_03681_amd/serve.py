@@ -44,6 +44,8 @@ def declare(lib) -> None:
     lib.nats_hybrid_attn_decode_tree.argtypes = [ctypes.POINTER(TreeParams)] + [vp] * 17 + [size, vp]
     lib.nats_hybrid_attn_tree_commit.restype = ctypes.c_int
     lib.nats_hybrid_attn_tree_commit.argtypes = [ctypes.POINTER(TreeParams)] + [vp] * 14
+    lib.nats_hybrid_attn_tree_commit_ex.restype = ctypes.c_int
+    lib.nats_hybrid_attn_tree_commit_ex.argtypes = [ctypes.POINTER(TreeParams)] + [vp] * 15
     lib.nats_cache_weights_workspace_bytes.restype = size
     lib.nats_cache_weights_workspace_bytes.argtypes = [ctypes.POINTER(CacheWeightsParams), ctypes.c_int32]
     lib.nats_cache_weights.restype = ctypes.c_int
@@ -139,11 +141,12 @@ def hybrid_attn_decode_tree(state, k_cache, v_cache, cache_len, q, k, v, alpha, 
 
 def hybrid_attn_tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, *,
                             linear_op: int = NATS_LINEAR_GDN, freeze_on_softmax: bool = False, k_nla=None, group: int = 1,
-                            err_flags=None, vis=None) -> torch.Tensor:
+                            err_flags=None, vis=None, n_nodes=None) -> torch.Tensor:
     """nats_hybrid_attn_tree_commit: the path to node [B] i32 (-1: nothing) is written into state, caches and cache_len, in place
-    -> vis [B,H*G,T] i32, the rows of the cache that each node of the path saw (0: not on the path)."""
+    -> vis [B,H*G,T] i32, the rows of the cache that each node of the path saw (0: not on the path).  n_nodes [B] i32, for padded
+    trees (nats_hybrid_attn_tree_commit_ex): a node from there on is none, like a number outside -1 .. T - 1 (err_flags: 2)."""
     lib = nb.load_library()
-    r = nb._host.tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, k_nla, vis, err_flags,
+    r = nb._host.tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, n_nodes, k_nla, vis, err_flags,
                              linear_op, freeze_on_softmax, group)
     if r is not None:
         if type(r) is int:
@@ -162,16 +165,17 @@ def hybrid_attn_tree_commit(state, k_cache, v_cache, cache_len, k, v, alpha, bet
     _require(mask, "mask", (B, H, T), torch.uint8)
     _require(parent, "parent", (B, T), torch.int32)
     _require(node, "node", (B,), torch.int32)
+    _require(n_nodes, "n_nodes", (B,), torch.int32)
     _require(k_nla, "k_nla", (B, HG, T, d), dt)
     _require(err_flags, "err_flags", (B, HG), torch.int32)
     vis = torch.empty((B, HG, T), dtype=torch.int32, device=v.device) if vis is None else vis
     _require(vis, "vis", (B, HG, T), torch.int32)
-    _require_here(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, k_nla, err_flags, vis)
+    _require_here(state, k_cache, v_cache, cache_len, k, v, alpha, beta, mask, parent, node, n_nodes, k_nla, err_flags, vis)
     p = TreeParams(B, H, T, d, cap, _dtype_code(k_cache), 0.0, 0.0, 0, 0.0, linear_op, int(freeze_on_softmax), group, None,
                    k_nla.data_ptr() if k_nla is not None else None)
-    _check(lib.nats_hybrid_attn_tree_commit(ctypes.byref(p), _ptr(state), _ptr(k_cache), _ptr(v_cache), _ptr(cache_len), _ptr(k),
-                                            _ptr(v), _ptr(alpha), _ptr(beta), _ptr(mask), _ptr(parent), _ptr(node), _ptr(vis),
-                                            _ptr(err_flags), _stream_ptr()))
+    _check(lib.nats_hybrid_attn_tree_commit_ex(ctypes.byref(p), _ptr(state), _ptr(k_cache), _ptr(v_cache), _ptr(cache_len), _ptr(k),
+                                               _ptr(v), _ptr(alpha), _ptr(beta), _ptr(mask), _ptr(parent), _ptr(n_nodes), _ptr(node),
+                                               _ptr(vis), _ptr(err_flags), _stream_ptr()))
     return vis
 
 
