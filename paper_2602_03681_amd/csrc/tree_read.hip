@@ -15,8 +15,8 @@
 //                                  joined by byte permutes (bf16) or stand as they came (fp32)
 // bf16 tensors: logits are exact products summed in fp32; P enters as the sum of three bf16 terms, all of its 24 bits: with two (17 bits) ten
 // times as many outputs were rounded to the wrong neighbour, and this kernel has matrix cycles to spare (us of a call with two / three: 1024
-// caches of 64 .. 2048 rows, 16 nodes 148 / 148; 32 of 32000, 64 nodes 130 / 130; 96 of 64 .. 1024, 33 nodes 27.5 / 28.2).  Every term is cut
-// off, so that the last one is exact, and the lower two are kept above 0, so that an infinity in V stays one.
+// caches of 64 .. 2048 rows, 16 nodes 148 / 148; 32 of 32000, 64 nodes 130 / 130, of 64 columns 82 / 87; 96 of 64 .. 1024, 33 nodes 27.5 / 28.2).
+// Every term is cut off, so that the last one is exact, and the lower two are kept above 0, so that an infinity in V stays one.
 #include <math.h>
 
 #include "mfma_util.h"
@@ -100,17 +100,20 @@ struct CacheTile<bf16_t, D> {
             float x = p[i / 2][2 * (i % 2)], y = p[i / 2][2 * (i % 2) + 1];
 #pragma unroll
             for (int n = 0; n < N_TERMS; ++n) {
-                const uint32_t hx = __float_as_uint(x) & 0xffff0000u, hy = __float_as_uint(y) & 0xffff0000u;
-                w[n][i] = (hx >> 16) | hy;
-                x = fmaxf(x - __uint_as_float(hx), 0x1p-120f);
-                y = fmaxf(y - __uint_as_float(hy), 0x1p-120f);
+                w[n][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);   // upper halves
+                if (n == N_TERMS - 1) break;
+                x = fmaxf(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u), 0x1p-120f);
+                y = fmaxf(y - __uint_as_float(__float_as_uint(y) & 0xffff0000u), 0x1p-120f);
             }
         }
     }
     // column `column(lq, j, e)` of the result is what element j of tile e holds
     __device__ __forceinline__ static int column(int lq, int j, int e) { return 2 * W * (4 * lq + j) + e; }
     template <int NQ>
-    __device__ __forceinline__ void products(const Weights (&w)[NQ], f32x4 (&o)[NQ][D / 16]) const {
+    __device__ __forceinline__ void products(const f32x4 (&p)[NQ][KT], f32x4 (&o)[NQ][D / 16]) const {
+        Weights w[NQ];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) weights(p[n], w[n]);
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) {
             u32x4 a;
@@ -129,7 +132,6 @@ template <int D>
 struct CacheTile<float, D> {
     static constexpr int KT = 1;
     using Query = float4[D / 16];
-    using Weights = f32x4[1];
     float4 k[D / 16];
     float4 v[4][D / 64];   // key 4 lq + j, columns 64 g + 4 l16 ..
     __device__ __forceinline__ static void load_query(const float* row, int lq, bool live, Query& q) {
@@ -165,20 +167,19 @@ struct CacheTile<float, D> {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) s[0] = mac16(k[i], q[i], s[0]);
     }
-    __device__ __forceinline__ static void weights(const f32x4 (&p)[KT], Weights& w) { w[0] = p[0]; }
     __device__ __forceinline__ static int column(int lq, int j, int e) { return 64 * (e / 4) + 16 * lq + 4 * j + e % 4; }
     template <int NQ>
-    __device__ __forceinline__ void products(const Weights (&w)[NQ], f32x4 (&o)[NQ][D / 16]) const {
+    __device__ __forceinline__ void products(const f32x4 (&p)[NQ][KT], f32x4 (&o)[NQ][D / 16]) const {
 #pragma unroll
         for (int g = 0; g < D / 64; ++g)
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    o[n][4 * g] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].x, w[n][0][j], o[n][4 * g], 0, 0, 0);
-                    o[n][4 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].y, w[n][0][j], o[n][4 * g + 1], 0, 0, 0);
-                    o[n][4 * g + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].z, w[n][0][j], o[n][4 * g + 2], 0, 0, 0);
-                    o[n][4 * g + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].w, w[n][0][j], o[n][4 * g + 3], 0, 0, 0);
+                    o[n][4 * g] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].x, p[n][0][j], o[n][4 * g], 0, 0, 0);
+                    o[n][4 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].y, p[n][0][j], o[n][4 * g + 1], 0, 0, 0);
+                    o[n][4 * g + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].z, p[n][0][j], o[n][4 * g + 2], 0, 0, 0);
+                    o[n][4 * g + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][g].w, p[n][0][j], o[n][4 * g + 3], 0, 0, 0);
                 }
             }
     }
@@ -233,7 +234,6 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
 #pragma unroll
         for (int i = 0; i < NQ; ++i) tile.logits(q[i], s[i]);
         tile.load_k(K, next, last, l16, lq);
-        typename Tile::Weights w[NQ];
         const bool whole = row + ROWS - 1 <= last;
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
@@ -265,10 +265,9 @@ __device__ __forceinline__ void tree_cache_block(const TreeCall& c, int bhg, int
                     s[i][t][j] = __builtin_amdgcn_exp2f(s[i][t][j] - ref);
                     l[i] += s[i][t][j];
                 }
-            Tile::weights(s[i], w[i]);
         }
         if (!whole) tile.clear_v(row, last, lq);
-        tile.template products<NQ>(w, o);
+        tile.template products<NQ>(s, o);
         tile.template load_v<QG == 1>(V, next, last, l16, lq);
     }
 #pragma unroll
@@ -374,8 +373,14 @@ __device__ __forceinline__ void tree_even_block(const TreeCall& c, int x, int he
     }
 }
 
+// Blocks of a CU that the registers are shared out for.  Narrow heads of bf16: four, or in equal shares of more than 16 nodes three, for with
+// the weights' three terms four leave some of the registers in memory (us of a call with four / three: 1024 caches of 64 .. 2048 rows, 20
+// nodes 97 / 92; 512 of them, 40 nodes 70 / 67; but without equal shares, where blocks are short, 300 caches of up to 1000 rows, 40 nodes
+// 34 / 37).
+constexpr int narrow_blocks(bool bf16, int T, bool even) { return bf16 && even && T > 16 ? 3 : 4; }
+
 template <typename T, int D, int NT, int TURNS, bool EVEN>
-__global__ __launch_bounds__(TC_THREADS, D == 64 ? 4 : 2) void tree_read_kernel(TreeCall c) {
+__global__ __launch_bounds__(TC_THREADS, D == 64 ? narrow_blocks(sizeof(T) == 2, 16 * NT, EVEN) : 2) void tree_read_kernel(TreeCall c) {
     constexpr int PARTS = D / (64 * TURNS);   // blocks of a head's linear branch
     constexpr int NQ = NT == 1 ? 1 : 2, QG = NT <= 2 ? 1 : 2;
     __shared__ union {
@@ -424,7 +429,7 @@ void tree_cache_parts(TreeCall& c) {
     c.rows = 2048;
     while (c.rows > 256 && heads * ((c.cap + c.rows - 1) / c.rows) < (c.rows > 512 ? 512 : 192)) c.rows /= 2;
     c.n_split = (c.cap + c.rows - 1) / c.rows;
-    const int per_cu = c.d == 64 ? (c.T <= 48 ? 4 : 2) : (c.T <= 16 ? 3 : 2);   // blocks that a CU holds
+    const int per_cu = c.d == 64 ? (c.T <= 48 ? narrow_blocks(c.dtype == NATS_BF16, c.T, true) : 2) : (c.T <= 16 ? 3 : 2);   // blocks that a CU holds
     c.even = !halves(c) && c.cap > 1024 && heads <= 2048 ? 256 * per_cu : 0;
 }
 
