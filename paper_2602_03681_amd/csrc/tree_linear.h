@@ -13,7 +13,8 @@
 // terms (all of its bits), the products with N, P and U, up to 64 x 64, on the fp32 one.
 //
 // In a product a node that is no ancestor has a coefficient of 0, which an infinity or a NaN in its u turns into NaN.  So a wavefront
-// whose u are not all finite does its columns again, ancestor by ancestor.
+// whose u are not all finite does its columns again, ancestor by ancestor.  And an infinity has no three terms that add up to it, nor has
+// a number that bf16 rounds to one: products of terms that are not all finite are formed again on the fp32 instruction.
 #pragma once
 #include "nats_common.h"
 #include "serve.h"
@@ -38,6 +39,12 @@ struct LinearLds {
 };
 
 __device__ __forceinline__ float4 as_float4(f32x4 x) { return make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ bool all_finite(f32x4 x) {
+    return fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY;
+}
+// four elements of a row as the fp32 instruction takes them
+__device__ __forceinline__ float4 row4(const float* p) { return ld4(p); }
+__device__ __forceinline__ float4 row4(const bf16_t* p) { return ldb4(reinterpret_cast<const uint16_t*>(p)); }
 
 // TURNS x 64 rows of S, number `part` of them
 template <typename T, int D, int NT, int TURNS>
@@ -133,6 +140,19 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
             kk[x] = mfma_terms(tk, tb, kk[x]);
             qk[x] = mfma_terms(tq, tb, qk[x]);
         }
+        if constexpr (sizeof(T) == 4) {
+            if (!__all(all_finite(kk[x]) && all_finite(qk[x]))) {
+                const int pair = wave + x * TL_WAVES, ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
+                const size_t i0 = (size_t)min(16 * ti + l16, N - 1) * D + 4 * lq, j0 = (size_t)min(16 * tj + l16, N - 1) * D + 4 * lq;
+                kk[x] = qk[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int i = 0; i < D; i += 16) {
+                    const float4 kj4 = row4(k + j0 + i);
+                    kk[x] = mac16(row4(k + i0 + i), kj4, kk[x]);
+                    qk[x] = mac16(row4(q + i0 + i), kj4, qk[x]);
+                }
+            }
+        }
     }
     __syncthreads();
     const bool plain = s.plain != 0;
@@ -174,7 +194,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         }
     }
     f32x4 w[NT], o[NT];
-    auto state_products = [&] {
+    auto state_products = [&](int row0) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -194,8 +214,25 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 o[t] = mfma_terms(tx, ts, o[t]);
             }
         }
+        bool fine = true;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) fine = fine && all_finite(w[t]) && all_finite(o[t]);
+        if (!__all(fine)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int i = 0; i < D; i += 16) {
+                const float4 s4 = ld4(S + (size_t)(row0 + l16) * D + i + 4 * lq);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const size_t at = (size_t)min(16 * t + l16, N - 1) * D + i + 4 * lq;
+                    w[t] = mac16(row4(k + at), s4, w[t]);
+                    o[t] = mac16(row4(q + at), s4, o[t]);
+                }
+            }
+        }
     };
-    state_products();
+    state_products(row0);
     __syncthreads();
 
     // ---- 16 columns at a time ----
@@ -205,7 +242,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         const int col = row0 + 16 * TL_WAVES * turn + l16;
         if (turn > 0) {
             load_values(col);
-            state_products();
+            state_products(row0 + 16 * TL_WAVES * turn);
         }
         if (turn + 1 < TURNS) load_state(row0 + 16 * TL_WAVES * (turn + 1));
         f32x4 u[NT];
