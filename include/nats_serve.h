@@ -2,7 +2,8 @@
  *
  * Conventions as in nats.h: device pointers owned by the caller, dense row-major tensors, 16-byte aligned data pointers, one
  * HIP stream, no allocation, no synchronisation, arguments checked on the host before anything is launched, no floating-point
- * atomics, calls that overlap in time need different workspaces.  Routing per token.  nats_abi_version() counts nats.h; what is
+ * atomics, calls that overlap in time need different workspaces.  What a call writes, its workspace included, shares no memory with
+ * anything else that it is given (NATS_ERR_SHAPE).  Routing per token.  nats_abi_version() counts nats.h; what is
  * declared here is found by name.
  *
  * A round of generation from drafts:

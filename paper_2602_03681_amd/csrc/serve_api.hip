@@ -20,6 +20,25 @@ static nats_status check_pointers(std::initializer_list<const void*> needed, con
     return NATS_OK;
 }
 
+// What a call writes, the first `written` arrays, must not share memory with anything else of the call.  (Arrays that are not given: NULL.)
+struct Span {
+    const char* name;
+    const void* p;
+    size_t n;   // bytes
+};
+static nats_status check_apart(std::initializer_list<Span> spans, int written) {
+    for (const Span* a = spans.begin(); a != spans.begin() + written; ++a)
+        for (const Span* b = a + 1; b != spans.end(); ++b) {
+            const uintptr_t pa = (uintptr_t)a->p, pb = (uintptr_t)b->p;
+            if (a->p != nullptr && b->p != nullptr && (pa < pb ? pb - pa < a->n : pa - pb < b->n)) {
+                set_error("%s must not share memory with %s", a->name, b->name);
+                return NATS_ERR_SHAPE;
+            }
+        }
+    return NATS_OK;
+}
+static size_t element(int dtype) { return dtype == NATS_F32 ? 4 : 2; }
+
 // sizes that all the operators share; the cache has H group heads
 static nats_status check_cache(int dtype, int B, int H, int d, int cap, int group) {
     if (dtype != NATS_F32 && dtype != NATS_BF16) {
@@ -126,6 +145,15 @@ nats_status nats_hybrid_attn_decode_tree(const nats_tree_params* p, const float*
         return NATS_ERR_WORKSPACE;
     }
     if (!aligned16(workspace)) { set_error("the workspace is not 16-byte aligned"); return NATS_ERR_ALIGN; }
+    const size_t es = element(c.dtype), nodes = (size_t)c.B * c.H * c.T, heads = (size_t)c.B * c.H * c.G, outs = nodes * c.G;
+    const size_t cache = heads * c.cap * c.d * es;
+    st = check_apart({{"o", o, outs * c.d * es}, {"lse", lse, 4 * outs}, {"the workspace", workspace, need},
+                      {"state", state, 4 * heads * c.d * c.d}, {"k_cache", k_cache, cache}, {"v_cache", v_cache, cache},
+                      {"cache_len", cache_len, 4 * heads}, {"q", q, nodes * c.d * es}, {"k", k, nodes * c.d * es}, {"v", v, outs * c.d * es},
+                      {"alpha", alpha, 4 * nodes}, {"beta", beta, 4 * nodes}, {"mask", mask, nodes}, {"parent", parent, 4 * (size_t)c.B * c.T},
+                      {"n_nodes", n_nodes, 4 * (size_t)c.B}, {"q_nla", p->q_nla, outs * c.d * es}, {"k_nla", p->k_nla, outs * c.d * es},
+                      {"w_nla", w_nla, 4 * outs}, {"w_la", w_la, 4 * outs}}, 3);
+    if (st != NATS_OK) return st;
     c.scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->d);
     c.la_scale = p->la_scale > 0.f ? p->la_scale : 1.0f;
     c.eps = p->rms_eps > 0.f ? p->rms_eps : 1e-6f;
@@ -162,6 +190,14 @@ nats_status nats_hybrid_attn_tree_commit_ex(const nats_tree_params* p, float* st
     c.state = state; c.k_cache = k_cache; c.v_cache = v_cache; c.cache_len = cache_len;
     c.k = k; c.v = v; c.k_nla = p->k_nla; c.alpha = alpha; c.beta = beta; c.mask = mask; c.parent = parent;
     c.n_nodes = n_nodes; c.node = node; c.vis = vis; c.err_flags = err_flags;
+    const size_t es = element(c.dtype), nodes = (size_t)c.B * c.H * c.T, heads = (size_t)c.B * c.H * c.G, outs = nodes * c.G;
+    const size_t cache = heads * c.cap * c.d * es;
+    st = check_apart({{"state", state, 4 * heads * c.d * c.d}, {"k_cache", k_cache, cache}, {"v_cache", v_cache, cache},
+                      {"cache_len", cache_len, 4 * heads}, {"vis", vis, 4 * outs}, {"err_flags", err_flags, 4 * heads},
+                      {"k", k, nodes * c.d * es}, {"v", v, outs * c.d * es}, {"alpha", alpha, 4 * nodes}, {"beta", beta, 4 * nodes},
+                      {"mask", mask, nodes}, {"parent", parent, 4 * (size_t)c.B * c.T}, {"n_nodes", n_nodes, 4 * (size_t)c.B},
+                      {"node", node, 4 * (size_t)c.B}, {"k_nla", p->k_nla, outs * c.d * es}}, 6);
+    if (st != NATS_OK) return st;
     return launch_tree_commit(c, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
@@ -200,6 +236,11 @@ nats_status nats_cache_weights(const nats_cache_weights_params* p, float* weight
         return NATS_ERR_WORKSPACE;
     }
     if (!aligned16(workspace)) { set_error("the workspace is not 16-byte aligned"); return NATS_ERR_ALIGN; }
+    const size_t es = element(c.dtype), heads = (size_t)c.B * c.H;
+    st = check_apart({{"weights", weights, 4 * heads * c.cap}, {"the workspace", need > 0 ? workspace : nullptr, need},
+                      {"q", q, heads / c.q_group * c.T * c.d * es}, {"k_cache", k_cache, heads * c.cap * c.d * es},
+                      {"cache_len", cache_len, 4 * heads}, {"vis", vis, 4 * heads / c.vis_group * c.T}, {"lse", lse, 4 * heads * c.T}}, 2);
+    if (st != NATS_OK) return st;
     c.weights = weights; c.q = q; c.k_cache = k_cache; c.cache_len = cache_len; c.vis = vis; c.lse = lse;
     c.ws = static_cast<float*>(workspace);
     return launch_cache_weights(c, reinterpret_cast<hipStream_t>(hip_stream));
@@ -218,6 +259,10 @@ static nats_status evict(const nats_cache_evict_params* p, void* k_cache, void* 
     st = check_pointers({k_cache, v_cache, weights}, "k_cache, v_cache and weights", {});
     if (st != NATS_OK) return st;
     if (k_cache == v_cache) { set_error("k_cache and v_cache must be two arrays"); return NATS_ERR_SHAPE; }
+    const size_t heads = (size_t)p->B * p->H, cache = heads * p->cap * p->d * element(p->dtype);
+    st = check_apart({{"k_cache", k_cache, cache}, {"v_cache", v_cache, cache}, {"cache_len", cache_len, 4 * heads},
+                      {"weights", weights, 4 * heads * p->cap}, {"kept", kept, 4 * heads * p->keep}}, 5);
+    if (st != NATS_OK) return st;
     EvictCall c{p->B, p->H, p->d, p->cap, p->dtype, p->keep, p->recent, k_cache, v_cache, cache_len, weights, kept, clear};
     return launch_cache_evict(c, reinterpret_cast<hipStream_t>(hip_stream));
 }
