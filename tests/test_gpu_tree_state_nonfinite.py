@@ -53,6 +53,22 @@ def test_an_infinity(dtype, d, T, linear_op, p):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [30, 1100])
+def test_an_infinity_in_many_heads(dtype, cap):
+    """More than 128 heads: a block takes 64 rows of the state, and then the others."""
+    x = ref.tree_inputs(10, 13, 5, 128, 30, DT[dtype], seed=7, own_qk=True, p=0.3)
+    for name in ("k_cache", "v_cache"):
+        rows = torch.zeros(10, 13, cap, 128, dtype=DT[dtype])
+        rows[:, :, :30] = x[name]
+        x[name] = rows
+    for h, row in enumerate((3, 40, 63, 64, 70, 100, 127)):
+        x["state"][h, 2 * h - 1, row, 17] = -math.inf
+    o, want = read(x, 1)
+    assert torch.isinf(want).sum() == 7 * 5
+    same(o, want, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("linear_op,p", [(0, 1.0), (1, 0.3)])
 def test_numbers_that_bf16_rounds_to_an_infinity(dtype, linear_op, p):
     """3.4e38, alone in its row: the product with the query is finite, and off by a few roundings of it."""
