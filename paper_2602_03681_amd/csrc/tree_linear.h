@@ -13,8 +13,8 @@
 // terms (all of its bits), the products with N, P and U, up to 64 x 64, on the fp32 one.
 //
 // In a product a node that is no ancestor has a coefficient of 0, which an infinity or a NaN in its u turns into NaN.  So a wavefront
-// whose u are not all finite does its columns again, ancestor by ancestor.  And an infinity has no three terms that add up to it, nor has
-// a number that bf16 rounds to one: products of terms that are not all finite are formed again on the fp32 instruction.
+// whose u and S q are not all finite does its columns again, ancestor by ancestor, with the products formed on the fp32 instruction: an infinity
+// has no three terms that add up to it, nor has a number that bf16 rounds to one.
 #pragma once
 #include "nats_common.h"
 #include "serve.h"
@@ -36,11 +36,16 @@ struct LinearLds {
     uint64_t anc[64];
     int par[64];
     int plain;                           // every decay is an ordinary positive number
+    int there;                           // nodes
 };
 
 __device__ __forceinline__ float4 as_float4(f32x4 x) { return make_float4(x[0], x[1], x[2], x[3]); }
-__device__ __forceinline__ bool all_finite(f32x4 x) {
-    return fabsf(x[0]) < INFINITY && fabsf(x[1]) < INFINITY && fabsf(x[2]) < INFINITY && fabsf(x[3]) < INFINITY;
+// four nodes' results, those of nodes from `first` up to `there` finite (what stands in nodes that are not there is of no use)
+__device__ __forceinline__ bool all_finite(f32x4 x, int first, int there) {
+    bool fine = true;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) fine = fine && (fabsf(x[e]) < INFINITY || first + e >= there);
+    return fine;
 }
 // four elements of a row as the fp32 instruction takes them
 __device__ __forceinline__ float4 row4(const float* p) { return ld4(p); }
@@ -122,7 +127,10 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
             s.b[lane] = bt;
             s.g[lane] = g;
             s.lg[lane] = lg;
-            if (lane == 0) s.plain = plain;
+            if (lane == 0) {
+                s.plain = plain;
+                s.there = there;
+            }
         }
     }
 
@@ -140,28 +148,30 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
             kk[x] = mfma_terms(tk, tb, kk[x]);
             qk[x] = mfma_terms(tq, tb, qk[x]);
         }
-        if constexpr (sizeof(T) == 4) {
-            if (!__all(all_finite(kk[x]) && all_finite(qk[x]))) {
-                const int pair = wave + x * TL_WAVES, ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
-                const size_t i0 = (size_t)min(16 * ti + l16, N - 1) * D + 4 * lq, j0 = (size_t)min(16 * tj + l16, N - 1) * D + 4 * lq;
-                kk[x] = qk[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-                for (int i = 0; i < D; i += 16) {
-                    const float4 kj4 = row4(k + j0 + i);
-                    kk[x] = mac16(row4(k + i0 + i), kj4, kk[x]);
-                    qk[x] = mac16(row4(q + i0 + i), kj4, qk[x]);
-                }
-            }
-        }
     }
     __syncthreads();
     const bool plain = s.plain != 0;
+    const int there = s.there;
 #pragma unroll
     for (int x = 0; x < PER_WAVE; ++x) {
         const int pair = wave + x * TL_WAVES;
         if (pair >= PAIRS) break;
         const int ti = tile_row(pair), tj = pair - ti * (ti + 1) / 2;
         const int j = 16 * tj + l16;
+        if constexpr (sizeof(T) == 4) {
+            // (node j is read as an ancestor, so it is there where the others are)
+            const int i0 = 16 * ti + 4 * lq;
+            if (!__all(j >= there || (all_finite(kk[x], i0, there) && all_finite(qk[x], i0, there)))) {
+                const size_t at = (size_t)min(16 * ti + l16, N - 1) * D + 4 * lq, up = (size_t)min(j, N - 1) * D + 4 * lq;
+                kk[x] = qk[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int i = 0; i < D; i += 16) {
+                    const float4 kj4 = row4(k + up + i);
+                    kk[x] = mac16(row4(k + at + i), kj4, kk[x]);
+                    qk[x] = mac16(row4(q + at + i), kj4, qk[x]);
+                }
+            }
+        }
         const double lgj = s.lg[j];
         const bool writes = s.b[j] != 0.f;
 #pragma unroll
@@ -175,8 +185,8 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 r = 1.f;
                 for (int m = i; m != j; m = s.par[m]) r *= s.a[m];
             }
-            // (a node that writes nothing: its key may hold anything)
-            s.n[i][j] = on && i != j && writes ? -s.b[i] * r * kk[x][e] : 0.f;
+            // (a node that writes nothing, as one that is not there: its key may hold anything)
+            s.n[i][j] = on && i != j && writes && s.b[i] != 0.f ? -s.b[i] * r * kk[x][e] : 0.f;
             s.p[i][j] = on && writes ? r * qk[x][e] : 0.f;
         }
     }
@@ -194,7 +204,7 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         }
     }
     f32x4 w[NT], o[NT];
-    auto state_products = [&](int row0) {
+    auto state_products = [&] {
 #pragma unroll
         for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -214,25 +224,22 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 o[t] = mfma_terms(tx, ts, o[t]);
             }
         }
-        bool fine = true;
+    };
+    auto state_products_again = [&](int row0) {   // on the fp32 instruction
 #pragma unroll
-        for (int t = 0; t < NT; ++t) fine = fine && all_finite(w[t]) && all_finite(o[t]);
-        if (!__all(fine)) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NT; ++t) w[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-            for (int i = 0; i < D; i += 16) {
-                const float4 s4 = ld4(S + (size_t)(row0 + l16) * D + i + 4 * lq);
+        for (int i = 0; i < D; i += 16) {
+            const float4 s4 = ld4(S + (size_t)(row0 + l16) * D + i + 4 * lq);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const size_t at = (size_t)min(16 * t + l16, N - 1) * D + i + 4 * lq;
-                    w[t] = mac16(row4(k + at), s4, w[t]);
-                    o[t] = mac16(row4(q + at), s4, o[t]);
-                }
+            for (int t = 0; t < NT; ++t) {
+                const size_t at = (size_t)min(16 * t + l16, N - 1) * D + i + 4 * lq;
+                w[t] = mac16(row4(k + at), s4, w[t]);
+                o[t] = mac16(row4(q + at), s4, o[t]);
             }
         }
     };
-    state_products(row0);
+    state_products();
     __syncthreads();
 
     // ---- 16 columns at a time ----
@@ -242,13 +249,12 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
         const int col = row0 + 16 * TL_WAVES * turn + l16;
         if (turn > 0) {
             load_values(col);
-            state_products(row0 + 16 * TL_WAVES * turn);
+            state_products();
         }
         if (turn + 1 < TURNS) load_state(row0 + 16 * TL_WAVES * (turn + 1));
         f32x4 u[NT];
         bool fine = true;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        auto weigh = [&](int t) {   // w: what the state alone has the nodes write; o: what they read of it
             const f32x4 g = *reinterpret_cast<const f32x4*>(&s.g[16 * t + 4 * lq]), bt = *reinterpret_cast<const f32x4*>(&s.b[16 * t + 4 * lq]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -256,14 +262,17 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
                 w[t][e] = bt[e] == 0.f ? 0.f : x;   // (a softmax token writes nothing, whatever its v)
                 o[t][e] *= g[e];
             }
+        };
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            weigh(t);
             u[t] = w[t];
             if (c.linear_op == 0) {
 #pragma unroll
                 for (int x = 0; x < t; ++x) u[t] = mac16(ld4(&s.n[16 * t + l16][16 * x + 4 * lq]), as_float4(u[x]), u[t]);
                 u[t] = mac16(ld4(&s.inv[t][l16][4 * lq]), as_float4(u[t]), f32x4{0.f, 0.f, 0.f, 0.f});
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) fine = fine && fabsf(u[t][e]) < INFINITY;
+            fine = fine && all_finite(u[t], 16 * t + 4 * lq, there) && all_finite(o[t], 16 * t + 4 * lq, there);
         }
         if (__all(fine)) {
 #pragma unroll
@@ -271,6 +280,10 @@ __device__ __forceinline__ void tree_linear_block(const TreeCall& c, int bhg, in
 #pragma unroll
                 for (int x = 0; x <= t; ++x) o[t] = mac16(ld4(&s.p[16 * t + l16][16 * x + 4 * lq]), as_float4(u[x]), o[t]);
         } else {
+            state_products_again(row0 + 16 * TL_WAVES * turn);
+            load_values(col);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) weigh(t);
             // ancestor by ancestor: 16 lanes a column each for u, then every lane its results
             float(&su)[16 * NT][16] = s.u[wave];
 #pragma unroll

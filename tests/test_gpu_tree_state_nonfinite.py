@@ -93,3 +93,24 @@ def test_an_infinite_query_of_a_root():
     o, want = read(x, 0)
     same(o, want, "f32")
     assert torch.isinf(o[:, :, 3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("linear_op,p", [(0, 1.0), (1, 0.3)])
+def test_an_infinity_beside_nodes_that_are_not_there(dtype, linear_op, p):
+    """The nodes behind n_nodes hold NaN; those before read the state's infinities as ever."""
+    x = ref.tree_inputs(3, 2, 24, 64, 30, DT[dtype], seed=13, own_qk=True, p=p)
+    nodes = torch.tensor([24, 11, 0], dtype=torch.int32)
+    x["state"][:, 0, 5, 9] = math.inf
+    x["state"][:, 1, 63, 0] = -math.inf
+    want, _ = ref.decode_tree(x, linear_op=linear_op, n_nodes=nodes)
+    for b in (1, 2):
+        for k in ("q", "k", "v", "q_nla", "k_nla", "alpha", "beta"):
+            x[k][b, :, int(nodes[b]):] = math.nan
+    g = {k: v.cuda() for k, v in x.items()}
+    o, _ = nats.hybrid_attn_decode_tree(*(g[k] for k in ARGS), q_nla=g["q_nla"], k_nla=g["k_nla"], linear_op=linear_op, n_nodes=nodes.cuda())
+    o = o.float().cpu()
+    fin = same(o, want, dtype)
+    assert torch.isinf(want[0, 0, :, 5]).all() and torch.isinf(want[1, 1, :11, 63]).all() and not o[2].any()
+    off = (o.double() - want)[fin].abs() - (torch.from_numpy(bf16_half_ulp(want[fin].numpy())) if dtype == "bf16" else 0.0)
+    assert float(off.max()) <= 8e-5 * float(want[fin].square().mean().sqrt())
